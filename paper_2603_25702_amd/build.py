@@ -9,7 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libs2d2.so")
-SOURCES = ["api.hip", "plan.hip", "elementwise.hip", "gemm.hip", "gemm_stream.hip", "gemm_mid.hip", "gemm_block.hip", "gemm_tile.hip", "gemm_lds.hip", "moe.hip", "attention.hip", "attention_wide.hip", "vocab.hip"]
+SOURCES = ["api.hip", "plan.hip", "elementwise.hip", "gemm.hip", "gemm_stream.hip", "gemm_mid.hip", "gemm_block.hip", "gemm_tile.hip", "gemm_lds.hip", "moe.hip", "attention.hip", "attention_wide.hip", "vocab.hip", "kv4_api.hip", "kv4_cache.hip", "kv4_attention.hip"]
 FLAGS = (["-DS2D2_KERNEL_TIMING"] if os.environ.get("S2D2_KERNEL_TIMING") else []) + ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -44,27 +44,28 @@ def build_lib(jobs: int = 6) -> str:
     return LIB
 
 
-def build_host_check() -> str:
-    """Builds tests/host/host_check: the library's objects with api.hip (all host-side argument checks and size
+HOST_CHECKED = ["api.hip", "kv4_api.hip"]   # entry points: host-side argument checks and size arithmetic
+
+
+def build_host_check(driver: str = "host_check") -> str:
+    """Builds tests/host/<driver>.cpp: the library's objects with the entry points (all host-side argument checks and size
     arithmetic) rebuilt under AddressSanitizer and UndefinedBehaviorSanitizer on the host side, linked with a driver
     that calls every entry point with extreme and invalid arguments.  Device code is not instrumented."""
     root = os.path.dirname(HERE)
-    out = os.path.join(HERE, "_build", "host_check")
-    objs = []
-    for src in SOURCES:
-        obj = os.path.join(HERE, "_build", src.replace(".hip", ".o"))
-        if src == "api.hip" or not os.path.exists(obj):
-            obj = _compile(src) if src != "api.hip" else obj
-        objs.append(obj)
+    out = os.path.join(HERE, "_build", driver)
+    plain = [s for s in SOURCES if s not in HOST_CHECKED]
+    objs = [os.path.join(HERE, "_build", s.replace(".hip", ".o")) for s in plain]
+    for src, obj in zip(plain, objs):
+        if not os.path.exists(obj):
+            _compile(src)
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined",
            "-Xarch_host", "-fno-omit-frame-pointer"]
-    api_san = os.path.join(HERE, "_build", "api_san.o")
-    drv = os.path.join(HERE, "_build", "host_check.o")
+    checked = [os.path.join(HERE, "_build", s.replace(".hip", "_san.o")) for s in HOST_CHECKED]
+    drv = os.path.join(HERE, "_build", driver + ".o")
     host_san = ["-fsanitize=address", "-fsanitize=undefined", "-fno-sanitize-recover=undefined"]
-    cmds = [[_hipcc(), *FLAGS, *san, "-c", os.path.join(CSRC, "api.hip"), "-o", api_san],
-            ["/opt/rocm/lib/llvm/bin/clang++", "-O1", "-g", "-std=c++17", *host_san, "-c", os.path.join(root, "tests", "host", "host_check.cpp"), "-o", drv],
-            [_hipcc(), "--offload-arch=gfx950", *host_san, "-fno-gpu-sanitize", drv, api_san,
-             *[o for o in objs if not o.endswith(os.sep + "api.o")], "-o", out]]
+    cmds = [[_hipcc(), *FLAGS, *san, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(HOST_CHECKED, checked)]
+    cmds += [["/opt/rocm/lib/llvm/bin/clang++", "-O1", "-g", "-std=c++17", *host_san, "-c", os.path.join(root, "tests", "host", driver + ".cpp"), "-o", drv],
+             [_hipcc(), "--offload-arch=gfx950", *host_san, "-fno-gpu-sanitize", drv, *checked, *objs, "-o", out]]
     for cmd in cmds:
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:

@@ -2,12 +2,15 @@
 // draft / verifier forward.  See include/s2d2.h for the contract of every entry point.
 #include "../../include/s2d2.h"
 #include "../../include/s2d2_aux.h"
+#include "../../include/s2d2_kv4.h"
 #include "s2d2_internal.h"
+#include "kv4.h"
 
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
 #include <stdarg.h>
+#include <math.h>
 #include <vector>
 #include <algorithm>
 
@@ -22,7 +25,7 @@ void launch_route(hipStream_t st, int N, int B, const s2d2_route_params& rp, con
                   uint64_t* unmask_fallback);
 }
 
-static int32_t fail(int32_t code, const char* fmt, ...) {
+int32_t s2d2::fail(int32_t code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
@@ -84,6 +87,11 @@ struct s2d2_ctx {
   unsigned long long* pair_buf;   // PAIR_CAP x 256 (value, tag) words of the streaming GEMM's paired K split, zero between launches
   int32_t prefetch_wgs;     // workgroups of the narrow attention launch that read the next two GEMMs' weights ahead
   int wide_wgs;             // workgroups the split choice of the wide attention kernel aims for
+  // prefix cache in 4 bits (s2d2_set_kv4)
+  bool kv4_on;
+  Kv4 kv4;
+  void* kv4_scratch;
+  float* kv4_lse;           // [rows_cap, Hq], with kv4.mass
   // profiling (measurement aid)
   bool prof_on;
   int32_t prof_cap;
@@ -267,6 +275,9 @@ int32_t check_kv(const s2d2_ctx* c, const s2d2_kv_view* kv) {
   if (!kv || !kv->k_pages || !kv->v_pages || !kv->page_table || !kv->seq_len) return fail(S2D2_EINVAL, "kv view or one of its pointers is NULL");
   if (kv->n_pages < 1 || kv->page_size < 1 || kv->max_pages_per_seq < 1) return fail(S2D2_EINVAL, "kv view: n_pages, page_size and max_pages_per_seq must be positive");
   if (((uintptr_t)kv->k_pages | (uintptr_t)kv->v_pages) & 15) return fail(S2D2_EINVAL, "kv pages must be 16-byte aligned");
+  if (c->kv4_on && (kv->k_pages != c->kv4.kc || kv->v_pages != c->kv4.vc || kv->page_table != c->kv4.page_table || kv->seq_len != c->kv4.seq_len ||
+                    kv->n_pages != c->kv4.n_pages || kv->page_size != c->kv4.ps.d || kv->max_pages_per_seq != c->kv4.max_pages))
+    return fail(S2D2_EINVAL, "the context keeps its prefix in a 4-bit cache (s2d2_set_kv4), which this kv view does not describe");
   return S2D2_OK;
 }
 
@@ -368,7 +379,9 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
   hipStream_t st = c->stream;
   const KvGeom g = geom(c, kv);
   // MFMA flash attention for bf16 / head_dim 128 / pages that hold whole 8-key groups; else the generic kernel
-  const bool flash = dt == S2D2_BF16 && d.head_dim == 128 && kv->page_size % 8 == 0;
+  const bool kv4 = c->kv4_on;   // the 4-bit cache has a kernel of its own for every shape
+  const bool flash = !kv4 && dt == S2D2_BF16 && d.head_dim == 128 && kv->page_size % 8 == 0;
+  const bool weigh = kv4 && c->kv4.mass && k_stage;   // forwards whose rows are staged for the cache
   const WideShape ws = wide_shape(c, kv, N, sz);
   const int q_tiles = ws.q_tiles;   // 32-row query tiles of this call's windows
   int Z = 1;
@@ -386,7 +399,7 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
       if (ws.tiles == 0) wide = false, Z = 1;
     }
   }
-  const size_t lds = flash ? 0 : attention_generic_lds_bytes(g, sz.win);
+  const size_t lds = flash || kv4 ? 0 : attention_generic_lds_bytes(g, sz.win);
   if (lds > 160 * 1024) return fail(S2D2_ENOSPC, "attention needs %zu bytes of LDS for max_pages_per_seq*page_size=%d keys (limit 163840)", lds, kv->max_pages_per_seq * kv->page_size);
   const size_t stage_layer = (size_t)c->rows_cap * d.n_kv_heads * d.head_dim * es;
   const size_t page_layer = (size_t)kv->n_pages * d.n_kv_heads * kv->page_size * d.head_dim * es;
@@ -400,7 +413,7 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
   // GEMM inputs: one plane of half values, in fragment order or in rows, or P bf16 planes per row ([hi | lo]); the low-plane offsets say which (0: one bf16 plane).  The plain kernels (no packed copy, or the generic attention) use one bf16 plane.
   // (the generic attention kernel reads and writes single planes: two-plane models then run on their high plane)
   const int mode = operand_mode_of(d);
-  const int opm = !fused ? OPM_BF16 : (flash || mode == OPM_F16 ? mode : OPM_BF16);
+  const int opm = !fused ? OPM_BF16 : (flash || kv4 || mode == OPM_F16 ? mode : OPM_BF16);
   const int P = opm == OPM_BF16X2 ? 2 : 1;
   const bool frag = fragment_order(d, opm, sz, env);
   auto lo_row = [&](int width) { return opm == OPM_F16 ? LO_F16 : (P == 2 ? width : 0); };   // rows of the MoE FFN
@@ -418,7 +431,7 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
   // model asked for single bf16 planes; the kernel for wide windows takes them as half values in the half mode
   // (it converts the keys and values on their way into LDS)
   const bool q_f16 = fused && wide && opm == OPM_F16;
-  const int PQ = fused && flash && opm != OPM_BF16 && !q_f16 ? 2 : 1;
+  const int PQ = fused && (flash || kv4) && opm != OPM_BF16 && !q_f16 ? 2 : 1;
   const int ld_q = PQ * HqD, lo_q = q_f16 ? LO_F16 : (PQ == 2 ? HqD : 0);
   if (fused) { ProfScope ps(c, 3, 0.0); launch_embed_norm(st, c->w.embed, d.d_model, c->plan, R, c->layers[0].norm1, c->h, c->a, ld_a, lo_a, c->ss, ss_stride, c->rope_cs, d.head_dim, d.rope_theta); }
   else { ProfScope ps(c, 3, 0.0); launch_embed_rmsnorm(st, dt, c->w.embed, d.d_model, c->plan, R, c->layers[0].norm1, d.rms_eps, d.head_dim, d.rope_theta, c->h, c->a, c->rope_cs); }
@@ -443,10 +456,20 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
       { ProfScope ps(c, 0, (double)qkv_n * d.d_model * es, fr * qkv_n * d.d_model, 4); launch_gemm(st, dt, EPI_STORE_F32, c->a, d.d_model, L.wqkv, d.d_model, qkv_n, n_rows, R, c->qkv, qkv_n); }
       { ProfScope ps(c, 3, 0.0); launch_rope_split(st, dt, c->qkv, c->plan, R, d.n_q_heads, d.n_kv_heads, d.head_dim, c->rope_cs, c->qbuf, kw, vw, flash ? c->vT_win : nullptr, c->wpad); }
     }
-    if (LR == 0 && l == d.n_layers - 1) return check_launch("forward");
+    if (LR == 0 && l == d.n_layers - 1 && !weigh) return check_launch("forward");
     const void* kp = (const uint8_t*)kv->k_pages + l * page_layer;
     const void* vp = (const uint8_t*)kv->v_pages + l * page_layer;
-    if (wide) {
+    if (kv4) {
+      Kv4Attn x{};
+      x.kv = c->kv4; x.N = N; x.T = sz.win; x.rows = R; x.Hq = d.n_q_heads; x.grp = d.n_q_heads / d.n_kv_heads; x.group = divisor_of(x.grp);
+      x.q = c->qbuf; x.q_ld = fused ? ld_q : HqD; x.q_lo = lo_q; x.k = kw; x.v = vw; x.kv_ld = (int64_t)d.n_kv_heads * d.head_dim;
+      x.row0 = c->plan.seq_row0; x.n_rows = c->plan.seq_rows; x.lo = c->plan.row_lo; x.hi = c->plan.row_hi;
+      x.out = c->obuf; x.o_ld = ld_o; x.o_lo = lo_o; x.lse = weigh ? c->kv4_lse : nullptr;
+      x.scale_log2e = 1.44269504088896340736f / sqrtf((float)d.head_dim);
+      { ProfScope ps(c, 1, 0.0); launch_kv4_attention(st, dt, PQ, x, l, c->kv4_scratch); }
+      if (weigh) { ProfScope ps(c, 1, 0.0); launch_kv4_weigh(st, dt, PQ, x, l); }
+      if (LR == 0 && l == d.n_layers - 1) return check_launch("forward");
+    } else if (wide) {
       { ProfScope ps(c, 1, 0.0); launch_attention_wide(st, c->qbuf, fused ? ld_q : HqD, fused ? lo_q : 0, q_f16 ? c->kwin16 : kw, c->vT_win, kp, vp, g, c->plan, N, d.n_q_heads, q_tiles, ws.per, ws.nw, Z, ws.target, ws.tiles, c->n_cus, c->wpad, c->obuf, ld_o, lo_o, c->attn_part, c->attn_part_entries); }
       if (Z > 1) { ProfScope ps(c, 1, 0.0); launch_attention_wide_merge(st, g, c->plan, N, d.n_q_heads, q_tiles, Z, c->obuf, ld_o, lo_o, c->attn_part, c->attn_part_entries); }
     } else if (flash) {
@@ -703,6 +726,26 @@ int32_t s2d2_set_stream(s2d2_ctx* ctx, void* stream) {
   return S2D2_OK;
 }
 
+int32_t s2d2_set_kv4(s2d2_ctx* c, const s2d2_kv4_view* kv, void* scratch, size_t scratch_bytes, float* lse) {
+  if (!c) return fail(S2D2_EINVAL, "ctx is NULL");
+  if (!kv) { c->kv4_on = false; return S2D2_OK; }
+  int32_t rc;
+  if ((rc = check_kv4(kv))) return rc;
+  const s2d2_model_desc& d = c->desc;
+  if (kv->n_layers != d.n_layers || kv->n_kv_heads != d.n_kv_heads || kv->head_dim != d.head_dim) return fail(S2D2_EINVAL, "4-bit cache of %d layers, %d KV heads, head_dim %d; the model has %d, %d, %d", kv->n_layers, kv->n_kv_heads, kv->head_dim, d.n_layers, d.n_kv_heads, d.head_dim);
+  const int64_t need = s2d2_kv4_attention_bytes(kv, c->max_batch, 3 * c->max_block, d.n_q_heads);
+  if (need < 0) return (int32_t)need;
+  if (scratch_bytes < (size_t)need) return fail(S2D2_ENOSPC, "scratch has %zu bytes, %lld needed", scratch_bytes, (long long)need);
+  if (need && (!scratch || ((uintptr_t)scratch & 15))) return fail(S2D2_EINVAL, "scratch is NULL or not 16-byte aligned");
+  if (kv->mass && (!lse || ((uintptr_t)lse & 3))) return fail(S2D2_EINVAL, "a cache with mass needs lse (fp32, s2d2_stage_rows() x n_q_heads)");
+  if ((rc = kv4_ready())) return rc;
+  c->kv4 = kv4_of(kv);
+  c->kv4_scratch = scratch;
+  c->kv4_lse = lse;
+  c->kv4_on = true;
+  return S2D2_OK;
+}
+
 static int32_t check_params(const s2d2_params* p) {
   if (!p) return fail(S2D2_EINVAL, "params is NULL");
   if (p->mode != S2D2_GREEDY && p->mode != S2D2_SAMPLE) return fail(S2D2_EINVAL, "unknown drafting mode %d", p->mode);
@@ -803,6 +846,20 @@ int32_t s2d2_accept_static(void* stream, int32_t vocab, const s2d2_block_state* 
   return check_launch("s2d2_accept_static");
 }
 
+// Appends lead[n] + accepted rows of the stage (those up to the last drafted token that has one) to the prefix cache; most: of one sequence.
+static void append_staged(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, int32_t most, const void* k_stage, const void* v_stage, const int32_t* row0,
+                          const int32_t* lead, const int32_t* span_len, const int32_t* n_accept, int hold_back) {
+  ProfScope ps(c, 3, 0.0);
+  const s2d2_model_desc& d = c->desc;
+  if (c->kv4_on) {
+    const int64_t width = (int64_t)d.n_kv_heads * d.head_dim;
+    launch_kv4_append(c->stream, d.dtype, c->kv4, N, Kv4Rows{row0, lead, n_accept, span_len, hold_back, most, c->rows_cap}, k_stage, v_stage, c->rows_cap * width, width);
+    return;
+  }
+  launch_kv_append(c->stream, d.dtype, d.n_layers, N, c->rows_cap, geom(c, kv), kv->k_pages, kv->v_pages, k_stage, v_stage, row0, lead, span_len, n_accept,
+                   kv->seq_len, kv->status, (most + 1) / 2, hold_back);
+}
+
 int32_t s2d2_kv_append(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, int32_t B, const s2d2_draft_out* draft,
                        const s2d2_verify_out* ver, const int32_t* n_accept) {
   int32_t rc;
@@ -810,10 +867,7 @@ int32_t s2d2_kv_append(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, int32_t B
   if (N < 1 || N > c->max_batch || B < 1 || B > c->max_block) return fail(S2D2_EINVAL, "N or B outside the limits given at create");
   if ((rc = check_kv(c, kv)) || (rc = check_draft_out(draft)) || (rc = check_verify_out(ver))) return rc;
   if (!n_accept) return fail(S2D2_EINVAL, "n_accept is NULL");
-  const KvGeom g = geom(c, kv);
-  { ProfScope ps(c, 3, 0.0); launch_kv_append(c->stream, c->desc.dtype, c->desc.n_layers, N, c->rows_cap, g, kv->k_pages, kv->v_pages,
-                   ver->k_stage, ver->v_stage, ver->stage_row0, ver->stage_lead, draft->span_len, n_accept,
-                   kv->seq_len, kv->status, B, c->desc.right_shifted); }
+  append_staged(c, kv, N, 2 * B, ver->k_stage, ver->v_stage, ver->stage_row0, ver->stage_lead, draft->span_len, n_accept, c->desc.right_shifted);
   return check_launch("s2d2_kv_append");
 }
 
@@ -829,11 +883,8 @@ int32_t s2d2_block_complete(s2d2_ctx* c, const s2d2_kv_view* kv, const s2d2_bloc
               nullptr, c->plan, scratch->logit_row_of, nullptr, nullptr, scratch->stage_row0, scratch->stage_lead, nullptr, nullptr,
               kv->max_pages_per_seq * kv->page_size, ws.target, ws.Z, ws.run); }
   if ((rc = forward(c, kv, N, verify_size(N, B, 0), scratch->k_stage, scratch->v_stage, scratch->logits_ver))) return rc;
-  const KvGeom g = geom(c, kv);
   // every staged row is appended: lead = rows, accepted = 0 (the zero array stands in for n_accept and span_len)
-  { ProfScope ps(c, 3, 0.0); launch_kv_append(c->stream, d.dtype, d.n_layers, N, c->rows_cap, g, kv->k_pages, kv->v_pages,
-                   scratch->k_stage, scratch->v_stage, scratch->stage_row0, scratch->stage_lead, c->zeros_i32, c->zeros_i32,
-                   kv->seq_len, kv->status, B, 0); }
+  append_staged(c, kv, N, 2 * B, scratch->k_stage, scratch->v_stage, scratch->stage_row0, scratch->stage_lead, c->zeros_i32, c->zeros_i32, 0);
   return check_launch("s2d2_block_complete");
 }
 
@@ -852,9 +903,7 @@ int32_t s2d2_prefill(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, int32_t T, 
   { ProfScope ps(c, 3, 0.0); launch_plan_prefill(c->stream, N, T, d.mask_id, kv->seq_len, tokens, ld, n_tokens, c->plan,
               kv->max_pages_per_seq * kv->page_size, ws.target, ws.Z, ws.run); }
   if ((rc = forward(c, kv, N, sz, k_stage, v_stage, nullptr))) return rc;
-  const KvGeom g = geom(c, kv);
-  { ProfScope ps(c, 3, 0.0); launch_kv_append(c->stream, d.dtype, d.n_layers, N, c->rows_cap, g, kv->k_pages, kv->v_pages,
-                   k_stage, v_stage, c->plan.seq_row0, c->plan.seq_lead, c->zeros_i32, c->zeros_i32, kv->seq_len, kv->status, (T + 1) / 2, 0); }
+  append_staged(c, kv, N, T, k_stage, v_stage, c->plan.seq_row0, c->plan.seq_lead, c->zeros_i32, c->zeros_i32, 0);
   return check_launch("s2d2_prefill");
 }
 

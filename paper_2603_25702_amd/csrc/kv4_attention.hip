@@ -1,0 +1,684 @@
+// Attention over the 4-bit cache and the windows' own rows, and the weights its entries gather.
+// Format and semantics: include/s2d2_kv4.h.
+#include "kv4.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace s2d2 {
+
+// ---------------------------------------------------------------------------------------------
+// kv4_attention_kernel: split-key attention on 32x32x16 MFMA.
+//
+// A query row is a (window row, query head of the group) pair, so a KV head's entries are read once for its group.  A
+// workgroup has one sequence, one KV head, QT tiles of 32 query rows and a run of tiles of 32 keys; its wavefronts take every NW-th of
+// them, each with a running maximum and sum of its own, and are merged at the end.
+//   S^T = K Q^T   the codes of a key become bf16 in the registers that the matrix instruction reads (v_cvt_scalef32_pk_bf16_fp4 applies the
+//                 group's power of two; every value is exact), so a lane holds one key's half row; the order of the dimensions in the
+//                 contraction is free and is the one that makes that half row contiguous in memory
+//   O^T = V^T P^T the contraction runs over keys while a lane holds one key: V goes through LDS as half values (exact as well) and
+//                 comes back transposed (ds_read_b64_tr_b16).  The rows of S^T are fed in an order that leaves the accumulators of a lane,
+//                 packed to half, as the operand P^T
+// A lane owns one query row (its column of S^T), so maximum, sum and scale need an exchange between two lanes only.  Scores are exponentiated
+// against a reference that lies 2^7 below the maximum it was taken from and follows the maximum when a weight would exceed 2^15: most
+// tiles rescale nothing, and half keeps 11 bits of a weight down to 2^-21 of the largest and 2^-32 of it below (with the maximum itself as the
+// reference a million entries of 2^-24 each would lose a tenth of their weights).  Sums are in 32 bits.
+// Operands of more than 16 bits (fp32 models; queries in two planes) are split into planes of bf16, whose products are exact in 32 bits: 3
+// planes hold the 24 bits of a float.  Softmax weights are half (11 bits; off by at most 2^-12 of the weight), of fp32 models two half planes.
+// The window's own rows, a few tiles, take the same way with K in the caller's type and V, weights in planes of bf16.
+// ---------------------------------------------------------------------------------------------
+static constexpr float LN2 = 0.69314718055994530942f;
+static constexpr float LOWEST = -3.402823466e38f;   // reference of a row that has seen nothing
+static constexpr float BELOW = 7.f, MOST = 15.f;    // a reference is taken this far below a maximum; scores exceed it by at most this (base 2)
+static constexpr int ATT_WAVES = 8;
+static constexpr int MIN_RUN = 32;                  // tiles of a split, at least: four a wavefront
+
+enum QueryMode { Q_BF16 = 0, Q_BF16X2 = 1, Q_F32 = 2 };
+template <int QM> struct Mode;
+// QP: planes of the queries; PP: of the softmax weights on cached values (half); WP: of the window's keys and values; WPP: of the weights on them (bf16)
+template <> struct Mode<Q_BF16> { typedef bf16_t T; static constexpr int QP = 1, PP = 1, WP = 1, WPP = 2; };
+template <> struct Mode<Q_BF16X2> { typedef bf16_t T; static constexpr int QP = 2, PP = 1, WP = 1, WPP = 2; };
+template <> struct Mode<Q_F32> { typedef float T; static constexpr int QP = 3, PP = 2, WP = 3, WPP = 3; };
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
+
+__device__ __forceinline__ int tile_key(int rr) {  // row of the score tile -> key of the tile of 32
+  const int a = rr >> 3, hh = (rr >> 2) & 1, b = rr & 3;
+  return (a >> 1) * 16 + hh * 8 + (a & 1) * 4 + b;
+}
+
+__device__ __forceinline__ f32x16_t mfma_bf16(const u32x4_t& a, const u32x4_t& b, const f32x16_t& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16_t mfma_f16(const u32x4_t& a, const u32x4_t& b, const f32x16_t& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
+// 8 codes at a group's power of two, as bf16 / half
+__device__ __forceinline__ u32x4_t codes_bf16(uint32_t w, float s) {
+  u32x4_t r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+  return r;
+}
+__device__ __forceinline__ u32x4_t codes_f16(uint32_t w, float s) {
+  u32x4_t r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
+  return r;
+}
+
+// 8 values as P planes of bf16 whose sum is the value (P = 3: exactly, above the subnormals)
+template <int P>
+__device__ __forceinline__ void split8(const float (&x)[8], u32x4_t (&p)[P]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      bf16x2_t h;
+      h[0] = (__bf16)a;
+      h[1] = (__bf16)b;
+      p[k][i] = __builtin_bit_cast(uint32_t, h);
+      if (k + 1 < P) { a -= (float)h[0]; b -= (float)h[1]; }
+    }
+  }
+}
+
+// 8 values of a row of the caller's type as P planes; lo: offset of a second plane, for P = 2
+template <int P>
+__device__ __forceinline__ void load_planes(const bf16_t* p, int lo, u32x4_t (&r)[P]) {
+  r[0] = *(const u32x4_t*)p;
+  if (P > 1) r[P - 1] = *(const u32x4_t*)(p + lo);
+}
+template <int P>
+__device__ __forceinline__ void load_planes(const float* p, int, u32x4_t (&r)[P]) {
+  const f32x4_t a = ((const f32x4_t*)p)[0], b = ((const f32x4_t*)p)[1];
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  split8<P>(x, r);
+}
+
+// ---- the batch as runs of key tiles ----
+struct SeqTiles { int rows, row0, S, cached, tiles; };   // tiles: cached and the window's own
+__device__ __forceinline__ SeqTiles seq_tiles(const Kv4Attn& a, int n) {
+  SeqTiles s{0, 0, 0, 0, 0};
+  if (n >= a.N) return s;
+  const int rows = max(0, min(a.n_rows[n], a.T)), row0 = a.row0[n], S = a.kv.held(n);
+  if (rows == 0 || row0 < 0 || row0 > a.rows - rows) return s;
+  s.rows = rows; s.row0 = row0; s.S = S;
+  s.cached = (S + 31) >> 5;
+  s.tiles = s.cached + (a.k ? (rows + 31) >> 5 : 0);
+  return s;
+}
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+// Tiles of a split: those of the whole batch over the workgroups that the launch aims for.
+__device__ __forceinline__ int run_length(const Kv4Attn& a, int lane) {
+  int total = 0;
+  for (int n0 = 0; n0 < a.N; n0 += 64) total += seq_tiles(a, n0 + lane).tiles;
+  const long long wanted = (long long)wave_sum(total) * a.per_item;
+  return max(MIN_RUN, (int)((wanted + a.target - 1) / a.target));
+}
+__device__ __forceinline__ int splits_of_seq(const SeqTiles& s, int run) { return s.rows == 0 ? 0 : max(1, (s.tiles + run - 1) / run); }
+
+// The sequence and split of item w; false: there is none.  All lanes of the wavefront, the same answer in each.
+struct Item { int n, z, splits, run; SeqTiles s; };
+__device__ __forceinline__ bool find_item(const Kv4Attn& a, int w, int lane, Item& it) {
+  it.run = run_length(a, lane);
+  int before = 0;
+  for (int n0 = 0; n0 < a.N; n0 += 64) {
+    const SeqTiles s = seq_tiles(a, n0 + lane);
+    const int mine = splits_of_seq(s, it.run);
+    int incl = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(incl, off, 64);
+      if (lane >= off) incl += y;
+    }
+    const unsigned long long hit = __ballot(w - before < incl && w - before >= incl - mine);
+    if (hit) {
+      const int src = __ffsll((long long)hit) - 1;
+      it.n = n0 + src;
+      it.splits = __builtin_amdgcn_readlane(mine, src);
+      it.z = w - before - (__builtin_amdgcn_readlane(incl, src) - it.splits);
+      it.s.rows = __builtin_amdgcn_readlane(s.rows, src);
+      it.s.row0 = __builtin_amdgcn_readlane(s.row0, src);
+      it.s.S = __builtin_amdgcn_readlane(s.S, src);
+      it.s.cached = __builtin_amdgcn_readlane(s.cached, src);
+      it.s.tiles = __builtin_amdgcn_readlane(s.tiles, src);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// Half a key's codes (dimensions half * D / 2 and on) and the scale bytes of its groups
+template <int D>
+struct HalfRow {
+  static constexpr int W = D / 16;                    // words of 8 codes
+  static constexpr int G = D >= 64 ? D / 64 : 1;      // groups
+  uint32_t w[W];
+  uint32_t scales;
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* sc, size_t at, int half) {
+    const uint8_t* p = codes + at * (D / 2) + half * (D / 4);
+    if (W == 2) { const uint2 x = *(const uint2*)p; w[0] = x.x; w[1] = x.y; }
+    else
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i) {
+        const uint4 x = ((const uint4*)p)[i];
+        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+      }
+    const uint8_t* q = sc + at * (D / 32) + (D >= 64 ? half * G : 0);
+    scales = G == 4 ? *(const uint32_t*)q : G == 2 ? *(const uint16_t*)q : *q;
+  }
+  __device__ __forceinline__ float scale(int word) const { return __uint_as_float(((scales >> (8 * (word / 4))) & 0xffu) << 23); }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0;
+    scales = 0x7f7f7f7fu;
+  }
+};
+
+// Scores of one tile (accumulators of a lane: query row c; keys 16 (i / 8) + 8 h + i % 8) into softmax weights against the row's
+// reference, which first follows the maximum if it has to.
+template <int D>
+struct RowState {
+  float m, l;            // l: of this lane's keys only
+  f32x16_t o[D / 32];
+  __device__ __forceinline__ void init() {
+    m = LOWEST;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  }
+  __device__ __forceinline__ void weights(const f32x16_t& s, float scale, float (&p)[16]) {
+    float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+#pragma unroll
+    for (int i = 3; i < 15; i += 2) mx = fmaxf(fmaxf(s[i], s[i + 1]), mx);
+    mx = fmaxf(mx, s[15]) * scale;
+    if (__ballot(mx > m + MOST)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float to = mx > m + MOST ? mx - BELOW : m, f = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
+      l += p[i];
+    }
+  }
+};
+
+template <int D>
+static constexpr int V_LD = 2 * D + 32;   // bytes of a key's row of V in LDS: 16 lanes of a transposing read touch four rows, which then lie in different banks
+
+template <int D, int QM, int QT>
+__global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4Attn a, int layer) {
+  typedef typename Mode<QM>::T T;
+  constexpr int QP = Mode<QM>::QP, PP = Mode<QM>::PP, WP = Mode<QM>::WP, WPP = Mode<QM>::WPP, NW = ATT_WAVES, DT = D / 32, DS = D / 16;
+  extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+  const Kv4& kv = a.kv;
+  // workgroups of one run of keys lie 8 apart: on one XCD, whose cache they share
+  const int groups = a.per_item / kv.H, wg = blockIdx.x;
+  const int qg = (wg >> 3) % groups, w = ((wg >> 3) / groups) * 8 + (wg & 7), kvh = w % kv.H;
+  Item it;
+  if (!find_item(a, w / kv.H, lane, it)) return;
+  const SeqTiles& sq = it.s;
+  const int nq = sq.rows * a.grp, q0 = qg * QT * 32;
+  if (q0 >= nq) return;
+  const int t0 = it.z * it.run, t1 = min(sq.tiles, t0 + it.run);
+  const int tiles_q = min(QT, (nq - q0 + 31) / 32);
+
+  // ---- queries: lane (c, h) has row c's dimensions h D / 2 + 8 ds .. + 7 for step ds ----
+  u32x4_t q[QT][DS][QP];
+  int row[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int qi = min(q0 + t * 32 + c, nq - 1), r = a.group.div(qi);
+    row[t] = sq.row0 + r;
+    const T* p = (const T*)a.q + row[t] * a.q_ld + (size_t)(kvh * a.grp + qi - r * a.grp) * D + h * (D / 2);
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) load_planes<QP>(p + 8 * ds, a.q_lo, q[t][ds]);
+  }
+  RowState<D> st[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) st[t].init();
+
+  uint8_t* s_v = s_mem + (size_t)wave * 32 * V_LD<D>;   // this wavefront's tile of V
+  const int kperm = tile_key(c);
+  const int g16 = lane >> 4, i16 = lane & 15;
+  // transposing read: 16 lanes take 16 dimensions of 4 keys; lanes 0-31 keys 0-7, lanes 32-63 keys 8-15 of a step
+  const uint8_t* s_tr = s_v + (8 * (g16 >> 1) + (i16 >> 2)) * V_LD<D> + ((g16 & 1) * 16 + (i16 & 3) * 4) * 2;
+  auto v_operand = [&](int dt, int j) __attribute__((always_inline)) {
+    const uint8_t* p = s_tr + 16 * j * V_LD<D> + dt * 64;
+    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)p), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(p + 4 * V_LD<D>));
+    const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
+    return u32x4_t{u.x, u.y, v.x, v.y};
+  };
+
+  // ---- cached keys ----
+  const int32_t* pt = kv.page_table + (size_t)it.n * kv.max_pages;
+  const uint8_t *kc = kv.kc + layer * kv.layer_entries * (D / 2), *vc = kv.vc + layer * kv.layer_entries * (D / 2);
+  const uint8_t *ks = kv.ks + layer * kv.layer_entries * (D / 32), *vs = kv.vs + layer * kv.layer_entries * (D / 32);
+  const int c1 = min(t1, sq.cached);
+  auto place_of = [&](int tile) __attribute__((always_inline)) { return min(tile * 32 + kperm, sq.S - 1); };
+  HalfRow<D> kn, vn;
+  int page_next = 0;
+  auto request_page = [&](int tile) __attribute__((always_inline)) { page_next = pt[kv.ps.div(place_of(tile))]; };
+  auto request = [&](int tile) __attribute__((always_inline)) {
+    const int key = place_of(tile), p = kv.ps.div(key), page = max(0, min(page_next, kv.n_pages - 1));
+    const size_t at = kv.at(page, kvh, key - p * kv.ps.d);
+    kn.load(kc, ks, at, h);
+    vn.load(vc, vs, at, h);
+  };
+  int tile = t0 + wave;
+  if (tile < c1) {
+    request_page(tile);
+    request(tile);
+    if (tile + NW < c1) request_page(tile + NW);
+  }
+  for (; tile < c1; tile += NW) {
+    const HalfRow<D> k = kn;
+    HalfRow<D> v = vn;
+    if (tile + NW < c1) {
+      request(tile + NW);
+      if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
+    }
+    const bool part = tile * 32 + 32 > sq.S;
+    if (part && tile * 32 + kperm >= sq.S) v.clear();   // (what lies behind the entries may be anything)
+#pragma unroll
+    for (int i = 0; i < DS; ++i) *(u32x4_t*)(s_v + kperm * V_LD<D> + h * D + 16 * i) = codes_f16(v.w[i], v.scale(i));
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    u32x4_t pw[QT][2][PP];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      f32x16_t s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) {
+        const u32x4_t kf = codes_bf16(k.w[ds], k.scale(ds));
+#pragma unroll
+        for (int p = 0; p < QP; ++p) s = mfma_bf16(kf, q[t][ds][p], s);
+      }
+      if (part) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = tile * 32 + 16 * (i >> 3) + 8 * h + (i & 7) < sq.S ? s[i] : -INFINITY;
+      }
+      float p[16];
+      st[t].weights(s, a.scale_log2e, p);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = p[8 * j + 2 * i], y = p[8 * j + 2 * i + 1];
+#pragma unroll
+          for (int e = 0; e < PP; ++e) {
+            f16x2_t hv;
+            hv[0] = (_Float16)x;
+            hv[1] = (_Float16)y;
+            pw[t][j][e][i] = __builtin_bit_cast(uint32_t, hv);
+            if (e + 1 < PP) { x -= (float)hv[0]; y -= (float)hv[1]; }
+          }
+        }
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const u32x4_t vf = v_operand(dt, j);
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int e = 0; e < PP; ++e) st[t].o[dt] = mfma_f16(vf, pw[t][j][e], st[t].o[dt]);
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // ---- the window's own keys: plane by plane ----
+  for (; tile < t1; tile += NW) {
+    const int base = (tile - sq.cached) * 32, key = base + kperm;
+    const bool there = key < sq.rows;
+    const int64_t at = (int64_t)(sq.row0 + min(key, sq.rows - 1)) * a.kv_ld + kvh * D + h * (D / 2);
+    u32x4_t kf[DS][WP], vf[DS][WP];
+    bool bad = false;   // a value of this key that is not finite: the rows that see it become NaN, the others must not
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) {
+      load_planes<WP>((const T*)a.k + at + 8 * ds, 0, kf[ds]);
+      load_planes<WP>((const T*)a.v + at + 8 * ds, 0, vf[ds]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad |= (vf[ds][0][i] & 0x7f80u) == 0x7f80u || (vf[ds][0][i] & 0x7f800000u) == 0x7f800000u;
+    }
+    bad |= (bool)__shfl_xor((int)bad, 32, 64);
+    const unsigned long long bad_at = __ballot(there && bad);   // bit c: key tile_key(c)
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+      for (int e = 0; e < WP; ++e)
+        if (!there || bad) vf[ds][e] = u32x4_t{0, 0, 0, 0};
+    u32x4_t pw[QT][2][WPP];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      f32x16_t s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+        for (int e = 0; e < WP; ++e)
+#pragma unroll
+          for (int p = 0; p < QP; ++p)
+            if (e + p < (QP > WP ? QP : WP)) s = mfma_bf16(kf[ds][e], q[t][ds][p], s);
+      const int lo = a.lo ? a.lo[row[t]] : sq.row0, hi = a.hi ? a.hi[row[t]] : row[t] + 1;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int rr = 8 * (i >> 2) + 4 * h + (i & 3), k = base + tile_key(rr), r = sq.row0 + k;
+        const bool seen = k < sq.rows && ((r >= lo && r < hi) || r == row[t]);
+        s[i] = !seen ? -INFINITY : (bad_at >> rr) & 1 ? NAN : s[i];
+      }
+      float p[16];
+      st[t].weights(s, a.scale_log2e, p);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float x[8] = {p[8 * j], p[8 * j + 1], p[8 * j + 2], p[8 * j + 3], p[8 * j + 4], p[8 * j + 5], p[8 * j + 6], p[8 * j + 7]};
+        split8<WPP>(x, pw[t][j]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < WP; ++e) {
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) *(u32x4_t*)(s_v + kperm * V_LD<D> + h * D + 16 * ds) = vf[ds][e];
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const u32x4_t vo = v_operand(dt, j);
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int p = 0; p < WPP; ++p)
+              if (e + p < WPP) st[t].o[dt] = mfma_bf16(vo, pw[t][j][p], st[t].o[dt]);
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+  // ---- the wavefronts' states into one, in a fixed order: the upper half of them deposits, the lower half adds, halved until one is left ----
+  constexpr int SLOT = 32 * D + 64;   // floats: output, maxima, sums
+  float* s_st = (float*)s_mem;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    st[t].l += __shfl_xor(st[t].l, 32, 64);
+    for (int half = NW / 2; half > 0; half >>= 1) {
+      __syncthreads();
+      if (wave >= half && wave < 2 * half) {
+        float* p = s_st + (size_t)(wave - half) * SLOT;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            ((float4*)p)[(dt * 4 + i) * 64 + lane] = make_float4(st[t].o[dt][4 * i], st[t].o[dt][4 * i + 1], st[t].o[dt][4 * i + 2], st[t].o[dt][4 * i + 3]);
+        if (h == 0) { p[32 * D + c] = st[t].m; p[32 * D + 32 + c] = st[t].l; }
+      }
+      __syncthreads();
+      if (wave < half) {
+        const float* p = s_st + (size_t)wave * SLOT;
+        const float m2 = p[32 * D + c], l2 = p[32 * D + 32 + c], to = fmaxf(st[t].m, m2);
+        const float f1 = __builtin_amdgcn_exp2f(st[t].m - to), f2 = __builtin_amdgcn_exp2f(m2 - to);
+        st[t].m = to;
+        st[t].l = st[t].l * f1 + l2 * f2;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 v = ((const float4*)p)[(dt * 4 + i) * 64 + lane];
+            st[t].o[dt][4 * i] = st[t].o[dt][4 * i] * f1 + v.x * f2;
+            st[t].o[dt][4 * i + 1] = st[t].o[dt][4 * i + 1] * f1 + v.y * f2;
+            st[t].o[dt][4 * i + 2] = st[t].o[dt][4 * i + 2] * f1 + v.z * f2;
+            st[t].o[dt][4 * i + 3] = st[t].o[dt][4 * i + 3] * f1 + v.w * f2;
+          }
+      }
+    }
+    if (wave == 0 && t < tiles_q) {
+      const int qi = q0 + t * 32 + c, head = kvh * a.grp + qi - a.group.div(min(qi, nq - 1)) * a.grp;
+      if (it.splits == 1) {
+        if (qi < nq) {
+          const float inv = st[t].l == 0.f ? 0.f : 1.f / st[t].l;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int d = head * D + dt * 32 + 8 * i + 4 * h;
+              const float x = st[t].o[dt][4 * i] * inv, y = st[t].o[dt][4 * i + 1] * inv, z = st[t].o[dt][4 * i + 2] * inv, u = st[t].o[dt][4 * i + 3] * inv;
+              if (QM == Q_F32) *(float4*)((float*)a.out + row[t] * a.o_ld + d) = make_float4(x, y, z, u);
+              else act_put4((bf16_t*)a.out, a.o_lo, row[t], d, (int)a.o_ld, x, y, z, u);
+            }
+          if (a.lse && h == 0) a.lse[(size_t)row[t] * a.Hq + head] = st[t].l == 0.f ? -INFINITY : (st[t].m + __builtin_amdgcn_logf(st[t].l)) * LN2;
+        }
+      } else {
+        // partial output in the accumulators' order, then maxima and sums
+        const size_t at = ((size_t)w * groups + qg) * QT + t;
+        float4* po = (float4*)(a.part_o + at * 32 * D);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            po[(dt * 4 + i) * 64 + lane] = make_float4(st[t].o[dt][4 * i], st[t].o[dt][4 * i + 1], st[t].o[dt][4 * i + 2], st[t].o[dt][4 * i + 3]);
+        if (h == 0) { a.part_ml[at * 64 + c] = st[t].m; a.part_ml[at * 64 + 32 + c] = st[t].l; }
+      }
+    }
+  }
+}
+
+// The splits of a (sequence, KV head, query tile) into its rows, in the order of the splits.
+template <int D, int QM>
+__global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int tiles, int per_wg) {
+  const Kv4& kv = a.kv;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int qt = blockIdx.x % tiles, kvh = (blockIdx.x / tiles) % kv.H, n = blockIdx.x / tiles / kv.H;
+  const int run = run_length(a, lane);
+  int first = 0;
+  for (int n0 = 0; n0 < n; n0 += 64) first += n0 + lane < n ? splits_of_seq(seq_tiles(a, n0 + lane), run) : 0;
+  first = wave_sum(first);
+  const SeqTiles sq = seq_tiles(a, n);
+  const int Z = splits_of_seq(sq, run), nq = sq.rows * a.grp;
+  if (Z < 2 || qt * 32 >= nq) return;
+  const int groups = a.per_item / kv.H, qg = qt / per_wg, t = qt % per_wg;
+  auto part = [&](int z) __attribute__((always_inline)) { return ((size_t)((first + z) * kv.H + kvh) * groups + qg) * per_wg + t; };
+  // element e (four outputs): lane 32 h + c, group e / 64 = dt * 4 + i
+  for (int e = tid; e < 8 * D; e += 256) {
+    const int c = e & 31, h = (e >> 5) & 1, g = e >> 6;
+    float m = LOWEST, l = 0.f;
+    for (int z = 0; z < Z; ++z) m = fmaxf(m, a.part_ml[part(z) * 64 + c]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z = 0; z < Z; ++z) {
+      const size_t at = part(z);
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 64 + c] - m);
+      const float4 v = ((const float4*)(a.part_o + at * 32 * D))[e];
+      l += f * a.part_ml[at * 64 + 32 + c];
+      o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+    }
+    const int qi = qt * 32 + c;
+    if (qi >= nq) continue;
+    const int r = a.group.div(qi), row = sq.row0 + r, head = kvh * a.grp + qi - r * a.grp, d = head * D + (g >> 2) * 32 + 8 * (g & 3) + 4 * h;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (QM == Q_F32) *(float4*)((float*)a.out + row * a.o_ld + d) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    else act_put4((bf16_t*)a.out, a.o_lo, row, d, (int)a.o_ld, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (a.lse && g == 0 && h == 0) a.lse[(size_t)row * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// kv4_weigh_kernel: the weights that a sequence's rows give its entries.  A workgroup has one sequence, one KV head and a run of key tiles, a
+// wavefront every NW-th tile.  Scores are computed as S = Q K^T, so that a lane owns a key and the sum over rows stays in it; the sums of a tile
+// over all query tiles are added to the mass once, by one lane a key, in a fixed order.
+// ---------------------------------------------------------------------------------------------
+template <int D, int QM>
+__global__ __launch_bounds__(64 * ATT_WAVES) void kv4_weigh_kernel(const Kv4Attn a, int layer) {
+  typedef typename Mode<QM>::T T;
+  constexpr int QP = Mode<QM>::QP, NW = ATT_WAVES, DS = D / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+  const Kv4& kv = a.kv;
+  const int kvh = blockIdx.x % kv.H;
+  Item it;
+  if (!find_item(a, blockIdx.x / kv.H, lane, it)) return;
+  const SeqTiles& sq = it.s;
+  const int nq = sq.rows * a.grp, t1 = min(sq.cached, (it.z + 1) * it.run);
+  const int32_t* pt = kv.page_table + (size_t)it.n * kv.max_pages;
+  const size_t layer0 = layer * kv.layer_entries;
+  for (int tile = it.z * it.run + wave; tile < t1; tile += NW) {
+    const int key = tile * 32 + c, k0 = min(key, sq.S - 1), p = kv.ps.div(k0), page = pt[p];
+    const size_t at = layer0 + kv.at(max(0, min(page, kv.n_pages - 1)), kvh, k0 - p * kv.ps.d);
+    HalfRow<D> k;
+    k.load(kv.kc, kv.ks, at, h);
+    u32x4_t kf[DS];
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) kf[ds] = codes_bf16(k.w[ds], k.scale(ds));
+    float sum = 0.f;
+    for (int q0 = 0; q0 < nq; q0 += 32) {
+      const int qi = min(q0 + c, nq - 1), r = a.group.div(qi);
+      const T* qp = (const T*)a.q + (sq.row0 + r) * a.q_ld + (size_t)(kvh * a.grp + qi - r * a.grp) * D + h * (D / 2);
+      // of row c: its lse to base 2, or what makes every weight 0
+      const float e = a.lse[(size_t)(sq.row0 + r) * a.Hq + kvh * a.grp + qi - r * a.grp];
+      const float mine = q0 + c >= nq || e == -INFINITY ? INFINITY : e * (1.f / LN2);
+      f32x16_t s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) {
+        u32x4_t qf[QP];
+        load_planes<QP>(qp + 8 * ds, a.q_lo, qf);
+#pragma unroll
+        for (int e2 = 0; e2 < QP; ++e2) s = mfma_bf16(qf[e2], kf[ds], s);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float ref = __shfl(mine, 8 * (i >> 2) + 4 * h + (i & 3), 64);
+        sum += ref == INFINITY ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2e, -ref));
+      }
+    }
+    sum += __shfl_xor(sum, 32, 64);
+    if (h == 0 && key < sq.S && page >= 0 && page < kv.n_pages) kv.mass[at] += sum;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------------------------
+static constexpr int TARGET = 512;   // workgroups of a launch: two a compute unit
+
+// Query tiles per workgroup: two share the conversion of K and V; one where there is no second, and where two would not leave registers.
+static int tiles_per_wg(int D, int dtype, int planes, int q_tiles) { return D <= 128 && dtype == S2D2_BF16 && planes == 1 && q_tiles >= 2 ? 2 : 1; }
+
+struct AttnShape { int q_tiles, per_wg, groups, items, most; };
+static AttnShape shape_of(const Kv4& kv, int dtype, int planes, int N, int T, int Hq, bool window) {
+  AttnShape s;
+  s.q_tiles = (T * (Hq / kv.H) + 31) / 32;
+  s.per_wg = tiles_per_wg(kv.D, dtype, planes, s.q_tiles);
+  s.groups = (s.q_tiles + s.per_wg - 1) / s.per_wg;
+  const int per_item = kv.H * s.groups;
+  // runs of the batch: at most the target, and one more a sequence; a sequence has no more than its pages hold
+  s.most = std::max(1, ((kv.cap + 31) / 32 + (window ? (T + 31) / 32 : 0) + MIN_RUN - 1) / MIN_RUN);
+  s.items = (int)std::min<long long>((long long)N * s.most, (TARGET + per_item - 1) / per_item + (long long)N);
+  return s;
+}
+
+// Enough for every smaller N and T as well: the target's workgroups, with two query tiles each at most, and one run a sequence, KV head and tile,
+// with what rounding up adds.
+size_t kv4_attention_bytes(const Kv4& kv, int N, int T, int Hq) {
+  const AttnShape s = shape_of(kv, S2D2_BF16, 1, N, T, Hq, true);
+  if (s.most < 2) return 0;
+  const size_t slots = 2 * TARGET + ((size_t)(N + 1) * kv.H + 8) * (s.q_tiles + 1);
+  return (slots * (32 * kv.D + 64) * sizeof(float) + 255) & ~(size_t)255;
+}
+
+template <int D>
+static constexpr size_t attn_lds() { return std::max((size_t)ATT_WAVES * 32 * V_LD<D>, (size_t)(ATT_WAVES / 2) * (32 * D + 64) * sizeof(float)); }
+
+template <int D, int QM, int QT>
+static void launch_attn(hipStream_t st, const Kv4Attn& a, int layer, const AttnShape& s) {
+  const int wgs = (a.items * a.kv.H + 7) / 8 * 8 * s.groups;
+  S2D2_LAUNCH((kv4_attention_kernel<D, QM, QT>), dim3(wgs), dim3(64 * ATT_WAVES), attn_lds<D>(), st, a, layer);
+  if (s.most > 1) S2D2_LAUNCH((kv4_merge_kernel<D, QM>), dim3(a.N * a.kv.H * s.q_tiles), dim3(256), 0, st, a, s.q_tiles, s.per_wg);
+}
+
+template <typename F>
+static void by_head_dim(int D, const F& f) {
+  if (D == 32) f(std::integral_constant<int, 32>{});
+  else if (D == 64) f(std::integral_constant<int, 64>{});
+  else if (D == 128) f(std::integral_constant<int, 128>{});
+  else f(std::integral_constant<int, 256>{});
+}
+
+void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int layer, void* scratch) {
+  const AttnShape s = shape_of(a.kv, dtype, planes, a.N, a.T, a.Hq, a.k != nullptr);
+  a.items = s.items;
+  a.per_item = a.kv.H * s.groups;
+  a.target = TARGET;
+  const size_t slots = (size_t)((s.items * a.kv.H + 7) / 8 * 8) * s.groups * s.per_wg;
+  a.part_o = (float*)scratch;
+  a.part_ml = a.part_o + slots * 32 * a.kv.D;
+  by_head_dim(a.kv.D, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    if (dtype == S2D2_F32) launch_attn<D, Q_F32, 1>(st, a, layer, s);
+    else if (planes == 2) launch_attn<D, Q_BF16X2, 1>(st, a, layer, s);
+    else if (D <= 128 && s.per_wg == 2) launch_attn<(D <= 128 ? D : 128), Q_BF16, 2>(st, a, layer, s);
+    else launch_attn<D, Q_BF16, 1>(st, a, layer, s);
+  });
+}
+
+void launch_kv4_weigh(hipStream_t st, int dtype, int planes, Kv4Attn& a, int layer) {
+  a.k = a.v = nullptr;
+  const AttnShape s = shape_of(a.kv, dtype, planes, a.N, a.T, a.Hq, false);
+  a.per_item = a.kv.H;
+  a.target = TARGET;
+  a.items = (int)std::min<long long>((long long)a.N * s.most, (TARGET + a.kv.H - 1) / a.kv.H + (long long)a.N);
+  by_head_dim(a.kv.D, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    const dim3 grid(a.items * a.kv.H), wg(64 * ATT_WAVES);
+    if (dtype == S2D2_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32>), grid, wg, 0, st, a, layer);
+    else if (planes == 2) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16X2>), grid, wg, 0, st, a, layer);
+    else S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16>), grid, wg, 0, st, a, layer);
+  });
+}
+
+// LDS above 64 KB has to be asked for, once a device.
+int kv4_attention_init() {
+  hipError_t e = hipSuccess;
+  auto limit = [&](const void* f, size_t bytes) { if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); };
+  for (int D : {32, 64, 128, 256})
+    by_head_dim(D, [&](auto dim) {
+      constexpr int D = decltype(dim)::value;
+      limit((const void*)kv4_attention_kernel<D, Q_BF16, 1>, attn_lds<D>());
+      limit((const void*)kv4_attention_kernel<D, Q_BF16X2, 1>, attn_lds<D>());
+      limit((const void*)kv4_attention_kernel<D, Q_F32, 1>, attn_lds<D>());
+      if (D <= 128) limit((const void*)kv4_attention_kernel<(D <= 128 ? D : 128), Q_BF16, 2>, attn_lds<(D <= 128 ? D : 128)>());
+    });
+  return e == hipSuccess ? 0 : -1;
+}
+
+}  // namespace s2d2

@@ -1,0 +1,335 @@
+// The 4-bit cache: quantising append, entries read back, eviction by gathered attention weight.
+// Format and semantics: include/s2d2_kv4.h.  All of it is bound by the bytes it moves.
+#include "kv4.h"
+
+namespace s2d2 {
+
+Kv4 kv4_of(const s2d2_kv4_view* view) {
+  const s2d2_kv4_view& w = *view;
+  Kv4 k;
+  k.kc = (uint8_t*)w.k_codes; k.vc = (uint8_t*)w.v_codes; k.ks = (uint8_t*)w.k_scales; k.vs = (uint8_t*)w.v_scales;
+  k.mass = w.mass; k.position = w.position; k.page_table = w.page_table; k.entries = w.entries; k.seq_len = w.seq_len; k.status = w.status;
+  k.n_layers = w.n_layers; k.n_pages = w.n_pages; k.max_pages = w.max_pages_per_seq; k.H = w.n_kv_heads; k.D = w.head_dim;
+  k.cap = w.max_pages_per_seq * w.page_size;
+  k.ps = divisor_of(w.page_size);
+  k.layer_entries = (size_t)w.n_pages * w.n_kv_heads * w.page_size;
+  return k;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Append.  A thread takes 8 values of a row (a 16-byte load of bf16), four neighbours make a group: the group's largest |x| goes round
+// by two DPP moves as an integer (the bits of |x| order as |x| does, with NaN above infinity above all else), v_cvt_scalef32_pk_fp4_f32
+// rounds x / 2^e to nearest-even codes.
+// ---------------------------------------------------------------------------------------------
+static constexpr int APPEND_ROWS = 4;   // rows of a sequence per workgroup
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if (sizeof(T) == 2) {
+    const uint4 r = *(const uint4*)p;
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  } else {
+    const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+}
+
+// Codes of the 8 values of this lane and the scale byte of its group (lanes 4 g .. 4 g + 3 hold a group).
+__device__ __forceinline__ uint32_t kv4_quantise(const float (&x)[8], uint32_t& scale) {
+  int a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = max(a, (int)(__float_as_uint(x[i]) & 0x7fffffffu));
+  a = max(a, __builtin_amdgcn_mov_dpp(a, 0xb1, 0xf, 0xf, true));
+  a = max(a, __builtin_amdgcn_mov_dpp(a, 0x4e, 0xf, 0xf, true));
+  const int e = kv4_exponent(__int_as_float(a));
+  const float s = __int_as_float((e + 127) << 23);
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
+  const bool bad = a >= 0x7f800000;
+  scale = bad ? 255u : (uint32_t)(e + 127);
+  return bad ? 0u : c;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4 kv, Kv4Rows r, int per_seq, const T* __restrict__ k, const T* __restrict__ v,
+                                                         int64_t layer_stride, int64_t row_stride) {
+  const int n = blockIdx.x / per_seq, l = blockIdx.y;
+  const int rows = r.count(n), S = kv.held(n), t0 = (blockIdx.x % per_seq) * APPEND_ROWS;
+  if (t0 >= rows || r.row0[n] > r.rows - rows || S + rows > kv.cap) return;   // (the commit flags a sequence without room)
+  const int pos0 = kv.seq_len[n], units = kv.H * kv.D / 8, per_head = kv.D / 8;
+  const int here = min(APPEND_ROWS, rows - t0);
+  const T* src[2] = {k + l * layer_stride + (r.row0[n] + t0) * row_stride, v + l * layer_stride + (r.row0[n] + t0) * row_stride};
+  for (int i = threadIdx.x; i < here * 2 * units; i += 256) {   // (a multiple of four: the lanes of a group stay together)
+    const int t = i / (2 * units), u = i % (2 * units), value = u >= units, w = u - value * units, head = w / per_head, part = w % per_head;
+    const int place = S + t0 + t, p = kv.ps.div(place);
+    const int page = kv.page_table[(size_t)n * kv.max_pages + p];
+    float x[8];
+    load8(src[value] + t * row_stride + (size_t)w * 8, x);
+    uint32_t scale;
+    const uint32_t codes = kv4_quantise(x, scale);
+    if (page < 0 || page >= kv.n_pages) continue;
+    const size_t at = l * kv.layer_entries + kv.at(page, head, place - p * kv.ps.d);
+    ((uint32_t*)((value ? kv.vc : kv.kc) + at * (kv.D / 2)))[part] = codes;
+    if ((part & 3) == 0) (value ? kv.vs : kv.ks)[at * (kv.D / 32) + part / 4] = (uint8_t)scale;
+    if (part == 0 && !value) {
+      if (kv.mass) kv.mass[at] = 0.f;
+      if (kv.position) kv.position[at] = pos0 + t0 + t;
+    }
+  }
+}
+
+__global__ void kv4_append_commit_kernel(Kv4 kv, Kv4Rows r, int N) {
+  const int n = blockIdx.x * blockDim.x + threadIdx.x;
+  if (n >= N) return;
+  const int rows = r.count(n), S = kv.held(n);
+  if (rows == 0 || r.row0[n] > r.rows - rows) return;
+  if (S + rows > kv.cap) {
+    if (kv.status) kv.status[n] = S2D2_ENOSPC;
+    return;
+  }
+  kv.entries[n] = S + rows;
+  kv.seq_len[n] += rows;
+}
+
+void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv4Rows& r, const void* k, const void* v, int64_t layer_stride, int64_t row_stride) {
+  const int per_seq = (r.most + APPEND_ROWS - 1) / APPEND_ROWS;
+  const dim3 grid(N * per_seq, kv.n_layers);
+  if (dtype == S2D2_BF16)
+    S2D2_LAUNCH(kv4_append_kernel<bf16_t>, grid, dim3(256), 0, st, kv, r, per_seq, (const bf16_t*)k, (const bf16_t*)v, layer_stride, row_stride);
+  else
+    S2D2_LAUNCH(kv4_append_kernel<float>, grid, dim3(256), 0, st, kv, r, per_seq, (const float*)k, (const float*)v, layer_stride, row_stride);
+  S2D2_LAUNCH(kv4_append_commit_kernel, dim3((N + 255) / 256), dim3(256), 0, st, kv, r, N);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Entries read back: 8 values a thread.
+// ---------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+template <typename T>
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4 kv, int N, int T_, const int32_t* __restrict__ first, T* __restrict__ k, T* __restrict__ v) {
+  const int n = blockIdx.x / T_, t = blockIdx.x % T_, l = blockIdx.y;
+  const int64_t place = (int64_t)first[n] + t;
+  if (place < 0 || place >= kv.held(n)) return;
+  const int p = kv.ps.div((int)place), units = kv.H * kv.D / 8, per_head = kv.D / 8;
+  const int page = max(0, min(kv.page_table[(size_t)n * kv.max_pages + p], kv.n_pages - 1));
+  for (int i = threadIdx.x; i < 2 * units; i += 256) {
+    const int value = i >= units, w = i - value * units, head = w / per_head, part = w % per_head;
+    const size_t at = l * kv.layer_entries + kv.at(page, head, (int)place - p * kv.ps.d);
+    const uint32_t c = ((const uint32_t*)((value ? kv.vc : kv.kc) + at * (kv.D / 2)))[part];
+    const float s = __int_as_float((int)(value ? kv.vs : kv.ks)[at * (kv.D / 32) + part / 4] << 23);   // (255: the conversion gives NaN)
+    const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+    const f32x2_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+    T* to = (value ? v : k) + (((size_t)l * N + n) * T_ + t) * kv.H * kv.D + (size_t)w * 8;
+    if (sizeof(T) == 2) {
+      // (exact: a code times a power of two has two significant bits)
+      auto two = [](f32x2_t x) { return (__float_as_uint(x[0]) >> 16) | (__float_as_uint(x[1]) & 0xffff0000u); };
+      *(uint4*)to = make_uint4(two(a), two(b), two(d), two(e));
+    } else {
+      ((float4*)to)[0] = make_float4(a[0], a[1], b[0], b[1]);
+      ((float4*)to)[1] = make_float4(d[0], d[1], e[0], e[1]);
+    }
+  }
+}
+
+void launch_kv4_read(hipStream_t st, int dtype, const Kv4& kv, int N, int T, const int32_t* first, void* k, void* v) {
+  const dim3 grid(N * T, kv.n_layers);
+  if (dtype == S2D2_BF16) S2D2_LAUNCH(kv4_read_kernel<bf16_t>, grid, dim3(256), 0, st, kv, N, T, first, (bf16_t*)k, (bf16_t*)v);
+  else S2D2_LAUNCH(kv4_read_kernel<float>, grid, dim3(256), 0, st, kv, N, T, first, (float*)k, (float*)v);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Eviction.  A workgroup per list (sequence, layer, KV head).  The list's masses become integers that order as they do (keys); three
+// histograms of 11, 11 and 10 bits find the key of the budget-th largest; of the entries that hold exactly that key the first ones
+// stay.  Entries below the budget that go are filled from those behind it that stay, in order: places that are written lie below the
+// budget, places that are read behind it, so the moves need no order among themselves, and a list that is a little too long moves a few
+// entries only.
+// A wavefront owns a run of consecutive entries in the walks that need ranks: its counts go through LDS once, ranks inside it
+// come from ballots.
+// ---------------------------------------------------------------------------------------------
+static constexpr int EVICT_KEYS = 32768;   // keys kept in LDS; those of longer lists are formed again from memory
+static constexpr int EVICT_MOVES = 2048;   // moves listed at a time
+static constexpr int EVICT_WAVES = 16;
+
+__device__ __forceinline__ uint32_t evict_key(float mass, int position, int sink, int tail) {
+  if (position < sink || position >= tail) return 0xffffffffu;
+  if (mass != mass) return 0u;
+  const uint32_t u = __float_as_uint(mass + 0.f);   // (-0 as 0)
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Sum over the workgroup's wavefronts before this one, and over all: `mine` of each wavefront (uniform in it).
+__device__ __forceinline__ int waves_before(int mine, int32_t* s /* [EVICT_WAVES] */, int& all) {
+  const int wave = threadIdx.x >> 6;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s[wave] = mine;
+  __syncthreads();
+  int before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < EVICT_WAVES; ++w) {
+    const int x = s[w];
+    before += w < wave ? x : 0;
+    all += x;
+  }
+  return before;
+}
+
+__global__ __launch_bounds__(64 * EVICT_WAVES) void kv4_evict_kernel(Kv4 kv, int budget, int slack, int sink, int recent, int keys) {
+  extern __shared__ uint32_t s_mem[];
+  uint32_t* s_key = s_mem;                         // [keys]
+  uint32_t* s_hist = s_key + keys;                 // [2048]
+  uint32_t* s_to = s_hist + 2048;                  // [EVICT_MOVES]
+  uint32_t* s_from = s_to + EVICT_MOVES;           // [EVICT_MOVES]
+  int32_t* s_sum = (int32_t*)(s_from + EVICT_MOVES);   // [EVICT_WAVES]
+  uint32_t* s_pick = (uint32_t*)(s_sum + EVICT_WAVES); // [2]
+  const int head = blockIdx.x % kv.H, n = blockIdx.x / kv.H, l = blockIdx.y;
+  const int E = kv.held(n);
+  if (E <= budget || E - budget <= slack) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t* pt = kv.page_table + (size_t)n * kv.max_pages;
+  const int tail = kv.seq_len[n] - recent;
+  // (a page outside the cache is read as the nearest one)
+  auto entry = [&](int i) __attribute__((always_inline)) {
+    const int p = kv.ps.div(i), page = max(0, min(pt[p], kv.n_pages - 1));
+    return l * kv.layer_entries + kv.at(page, head, i - p * kv.ps.d);
+  };
+  auto form = [&](int i) __attribute__((always_inline)) {
+    const size_t at = entry(i);
+    return evict_key(kv.mass[at], kv.position[at], sink, tail);
+  };
+  auto key = [&](int i) __attribute__((always_inline)) { return i < keys ? s_key[i] : form(i); };
+
+  // ---- the budget-th largest key ----
+  uint32_t prefix = 0;
+  int need = budget;   // among the keys with this prefix
+  int shift = 32;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int bits = pass < 2 ? 11 : 10;
+    for (int i = tid; i < 2048; i += 64 * EVICT_WAVES) s_hist[i] = 0;
+    __syncthreads();
+    for (int i0 = 0; i0 < E; i0 += 64 * EVICT_WAVES) {
+      const int i = i0 + tid;
+      bool counts = i < E;
+      uint32_t k = 0;
+      if (counts) {
+        k = pass == 0 ? form(i) : key(i);
+        if (pass == 0 && i < keys) s_key[i] = k;
+        counts = pass == 0 || (k >> shift) == prefix;
+      }
+      const int bin = (int)((k >> (shift - bits)) & ((1u << bits) - 1));
+      // entries without weight share a bin: the lanes that agree with the first one add once
+      const unsigned long long who = __ballot(counts);
+      if (who) {
+        const int lead = __ffsll((long long)who) - 1, first = __builtin_amdgcn_readlane(bin, lead);
+        const unsigned long long same = __ballot(counts && bin == first);
+        if (lane == lead) atomicAdd(&s_hist[first], (uint32_t)__popcll(same));
+        else if (counts && bin != first) atomicAdd(&s_hist[bin], 1u);
+      }
+    }
+    __syncthreads();
+    // counts from the top: thread t holds bins 2047 - 2 t and 2046 - 2 t
+    const int b = 2047 - 2 * tid;
+    const int x0 = (int)s_hist[b], x1 = (int)s_hist[b - 1];
+    int incl = x0 + x1;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(incl, off, 64);
+      if (lane >= off) incl += y;
+    }
+    int all;
+    const int above = waves_before(__builtin_amdgcn_readlane(incl, 63), s_sum, all) + incl - x0 - x1;
+    if (above < need && above + x0 >= need) { s_pick[0] = b; s_pick[1] = need - above; }
+    else if (above + x0 < need && above + x0 + x1 >= need) { s_pick[0] = b - 1; s_pick[1] = need - above - x0; }
+    __syncthreads();
+    shift -= bits;
+    prefix = (prefix << bits) | s_pick[0];
+    need = (int)s_pick[1];
+  }
+  const uint32_t last = prefix;   // of the entries with this key the first `need` stay
+
+  // ---- who stays: wavefront w walks entries [w0, w1) ----
+  const int run = ((E + 64 * EVICT_WAVES - 1) / (64 * EVICT_WAVES)) * 64, w0 = min(E, wave * run), w1 = min(E, w0 + run);
+  auto lanes_below = [&](unsigned long long m) __attribute__((always_inline)) { return __popcll(m & ((1ull << lane) - 1)); };
+  int equal = 0, all;
+  for (int i = w0 + lane; i - lane < w1; i += 64) equal += __popcll(__ballot(i < w1 && key(i) == last));
+  const int equal0 = waves_before(equal, s_sum, all);
+  // calls put(entry, whether it stays) for the wavefront's entries in order, all lanes together
+  auto walk = [&](auto put) __attribute__((always_inline)) {
+    int seen = equal0;
+    for (int i = w0 + lane; i - lane < w1; i += 64) {
+      const bool in = i < w1;
+      const uint32_t k = in ? key(i) : 0u;
+      const unsigned long long eq = __ballot(in && k == last);
+      const bool stays = in && (k > last || (k == last && seen + lanes_below(eq) < need));
+      seen += __popcll(eq);
+      put(i, in, stays);
+    }
+  };
+  int holes = 0, kept = 0;
+  walk([&](int i, bool in, bool stays) __attribute__((always_inline)) {
+    holes += __popcll(__ballot(in && i < budget && !stays));
+    kept += __popcll(__ballot(stays && i >= budget));
+  });
+  int moves;
+  const int holes0 = waves_before(holes, s_sum, moves), kept0 = waves_before(kept, s_sum, all);
+  moves = min(moves, all);   // (the same number)
+
+  // ---- the moves, so many at a time ----
+  const int codes = kv.D / 32, items = 2 * codes + 4, width = items <= 8 ? 8 : items <= 16 ? 16 : 32;   // 16-byte pieces of K and V; scales, mass, position
+  for (int m0 = 0; m0 < moves; m0 += EVICT_MOVES) {
+    __syncthreads();
+    int hole = holes0 - m0, keep = kept0 - m0;
+    walk([&](int i, bool in, bool stays) __attribute__((always_inline)) {
+      const unsigned long long goes = __ballot(in && i < budget && !stays), comes = __ballot(stays && i >= budget);
+      const int a = hole + lanes_below(goes), b = keep + lanes_below(comes);
+      if (in && i < budget && !stays && a >= 0 && a < EVICT_MOVES) s_to[a] = i;
+      if (stays && i >= budget && b >= 0 && b < EVICT_MOVES) s_from[b] = i;
+      hole += __popcll(goes);
+      keep += __popcll(comes);
+    });
+    __syncthreads();
+    const int now = min(EVICT_MOVES, moves - m0), j = tid % width;
+    for (int m = tid / width; m < now; m += 64 * EVICT_WAVES / width) {
+      const int to = (int)s_to[m];
+      const int page = pt[kv.ps.div(to)];
+      if (page < 0 || page >= kv.n_pages) continue;
+      const size_t a = entry(to), b = entry((int)s_from[m]);
+      if (j < 2 * codes) {
+        uint8_t* base = j < codes ? kv.kc : kv.vc;
+        const int piece = j < codes ? j : j - codes;
+        ((uint4*)(base + a * (kv.D / 2)))[piece] = ((const uint4*)(base + b * (kv.D / 2)))[piece];
+      } else if (j < 2 * codes + 2) {
+        uint8_t* base = j == 2 * codes ? kv.ks : kv.vs;
+        for (int g = 0; g < codes; ++g) base[a * codes + g] = base[b * codes + g];
+      } else if (j == 2 * codes + 2) kv.mass[a] = kv.mass[b];
+      else if (j == 2 * codes + 3) kv.position[a] = kv.position[b];
+    }
+  }
+}
+
+__global__ void kv4_evict_commit_kernel(Kv4 kv, int N, int budget, int slack) {
+  const int n = blockIdx.x * blockDim.x + threadIdx.x;
+  if (n >= N) return;
+  const int E = kv.held(n);
+  if (E > budget && E - budget > slack) kv.entries[n] = budget;
+}
+
+static size_t evict_lds(int keys) { return ((size_t)keys + 2048 + 2 * EVICT_MOVES + EVICT_WAVES + 2) * sizeof(uint32_t); }
+
+void launch_kv4_evict(hipStream_t st, const Kv4& kv, int N, int budget, int slack, int sink, int recent) {
+  const int keys = kv.cap < EVICT_KEYS ? kv.cap : EVICT_KEYS;
+  S2D2_LAUNCH(kv4_evict_kernel, dim3(N * kv.H, kv.n_layers), dim3(64 * EVICT_WAVES), evict_lds(keys), st, kv, budget, slack, sink, recent, keys);
+  S2D2_LAUNCH(kv4_evict_commit_kernel, dim3((N + 255) / 256), dim3(256), 0, st, kv, N, budget, slack);
+}
+
+// LDS above 64 KB has to be asked for, once a device.
+int kv4_evict_init() {
+  return hipFuncSetAttribute((const void*)kv4_evict_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)evict_lds(EVICT_KEYS)) != hipSuccess;
+}
+
+}  // namespace s2d2

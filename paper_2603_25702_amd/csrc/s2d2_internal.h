@@ -21,6 +21,8 @@ extern thread_local hipEvent_t g_prof_start, g_prof_stop;
     }                                                                                                          \
   } while (0)
 
+int32_t fail(int32_t code, const char* fmt, ...);   // sets the text of s2d2_last_error and returns the code (api.hip)
+
 typedef uint16_t bf16_t;  // raw bfloat16 bits
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;

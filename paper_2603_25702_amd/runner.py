@@ -12,14 +12,26 @@ import torch
 import dataclasses
 
 from .binding import AcceptOut, BlockState, DraftOut, Engine, KvCache, Params, RouteOut, RouteParams, VerifyOut
+from .kv4 import Kv4Cache, s2d2_kv4_evict, s2d2_set_kv4
 
 PREFILL_BLOCK = 64  # least max_block of a session's workspace: a prefill forward takes 3 * max_block tokens of every sequence
 
 
 class Session:
+    """cache_bits = 4 keeps the prefix in a 4-bit cache (include/s2d2_kv4.h).  With a budget that cache is bounded: after every append, and
+    between the chunks of a prompt, a sequence with more than budget + slack entries keeps `budget` of them in every layer and KV head, the first
+    `sink` and the last `recent` positions and those that gathered the most attention weight; max_seq then is the room for
+    budget + slack entries and the rows of one append."""
+
     def __init__(self, cfg, weights: Dict[str, torch.Tensor], N: int, B: int, max_seq: int, page_size: int = 16,
                  device: str = "cuda:0", page_table: Optional[np.ndarray] = None, max_block: Optional[int] = None,
-                 act_planes: int = 0):
+                 act_planes: int = 0, cache_bits: int = 16, budget: Optional[int] = None, slack: int = 0, sink: int = 4,
+                 recent: int = 0):
+        if cache_bits not in (4, 16) or (budget is not None and cache_bits != 4):
+            raise ValueError("cache_bits is 16 (the model's own type) or 4, and only a 4-bit cache has a budget")
+        if budget is not None and not (budget >= 1 and slack >= 0 and sink >= 0 and recent >= 0 and sink + recent <= budget):
+            raise ValueError("a budget is positive, slack, sink and recent are not negative, and sink + recent fit in the budget")
+        self.bound = None if budget is None else (budget, slack, sink, recent)
         self.cfg, self.N, self.B = cfg, N, B
         self.dev = torch.device(device)
         self.eng = Engine(cfg, weights, N, max_block or max(B, PREFILL_BLOCK), device, act_planes=act_planes)
@@ -28,12 +40,16 @@ class Session:
         if page_table is None:
             page_table = np.arange(N * max_pages, dtype=np.int32).reshape(N, max_pages)
         n_pages = int(page_table.max()) + 1
-        shape = (cfg.n_layers, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim)
-        vshape = (cfg.n_layers, n_pages, cfg.n_kv_heads, cfg.head_dim, page_size)  # V is cached key-minor
-        self.kv = KvCache(torch.zeros(shape, dtype=cfg.torch_dtype, device=self.dev),
-                          torch.zeros(vshape, dtype=cfg.torch_dtype, device=self.dev),
-                          torch.as_tensor(page_table, dtype=i32, device=self.dev),
-                          torch.zeros(N, dtype=i32, device=self.dev), torch.zeros(N, dtype=i32, device=self.dev))
+        table = torch.as_tensor(page_table, dtype=i32, device=self.dev)
+        if cache_bits == 4:
+            self.kv = Kv4Cache.alloc(cfg.n_layers, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim, table, weights=budget is not None)
+            s2d2_set_kv4(self.eng, self.kv)
+        else:
+            shape = (cfg.n_layers, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim)
+            vshape = (cfg.n_layers, n_pages, cfg.n_kv_heads, cfg.head_dim, page_size)  # V is cached key-minor
+            self.kv = KvCache(torch.zeros(shape, dtype=cfg.torch_dtype, device=self.dev),
+                              torch.zeros(vshape, dtype=cfg.torch_dtype, device=self.dev), table,
+                              torch.zeros(N, dtype=i32, device=self.dev), torch.zeros(N, dtype=i32, device=self.dev))
         mb = self.eng.max_block
         self._blk = torch.full((N, mb), cfg.mask_id, dtype=i32, device=self.dev)
         self._car = torch.zeros((N, mb), dtype=i32, device=self.dev)
@@ -43,6 +59,10 @@ class Session:
         self.a = self.eng.alloc_accept_out(N, B)
         self.step_dev = torch.zeros(1, dtype=i32, device=self.dev)
         self.st = self._state(B)
+
+    @property
+    def four(self) -> bool:
+        return isinstance(self.kv, Kv4Cache)
 
     def _state(self, B: int) -> BlockState:
         # [N, B] views over the front of flat storage, so any B <= max_block is contiguous
@@ -54,20 +74,32 @@ class Session:
         3 * max_block tokens of every sequence (equal chunks), all enqueued without a wait in between."""
         N, most = self.N, 3 * self.eng.max_block
         lens = [len(x) for x in ids]
-        longest = max(lens)
+        last = [int(x[-1]) for x in ids]
+        if self.four and getattr(self.cfg, "right_shifted", False):   # (the carried last token gets no entry: there may be no telling which one it is)
+            ids = [x[:-1] for x in ids]
+        cached = [len(x) for x in ids]
+        longest = max(cached)
         self.kv.seq_len.zero_()
+        if self.four:
+            self.kv.entries.zero_()
         if longest:
             chunks = (longest + most - 1) // most
             T = (longest + chunks - 1) // chunks
             host = np.zeros((N, chunks * T), dtype=np.int32)
             for n in range(N):
-                host[n, :lens[n]] = ids[n]
-            left = np.clip(np.asarray(lens)[None, :] - T * np.arange(chunks)[:, None], 0, T).astype(np.int32)
+                host[n, :cached[n]] = ids[n]
+            left = np.clip(np.asarray(cached)[None, :] - T * np.arange(chunks)[:, None], 0, T).astype(np.int32)
             tok, n_tok = torch.from_numpy(host).to(self.dev), torch.from_numpy(left).to(self.dev)
             for c in range(chunks):
                 self.eng.s2d2_prefill(self.kv, N, T, tok, c * T, n_tok[c], self.v.k_stage, self.v.v_stage)
+                self._evict()
         torch.cuda.synchronize(self.dev)
-        self.reset_blocks(lens, [int(x[-1]) for x in ids])
+        if self.four and int(self.kv.status.abs().sum()):
+            raise RuntimeError(f"prefill: device status {self.kv.status.cpu().tolist()}: the cache has no room for a chunk of {T} tokens")
+        entries = self.kv.entries.clone() if self.four else None
+        self.reset_blocks(lens, last)
+        if self.four:
+            self.kv.entries.copy_(entries)
 
     def reset_blocks(self, seq_lens: Sequence[int], last_tokens: Optional[Sequence[int]] = None):
         """Fresh [MASK]^B block right after the prefix of every sequence.  For a right-shifted model the last prefix
@@ -84,8 +116,15 @@ class Session:
             self.st.carry_tokens[:, 0].copy_(torch.as_tensor(list(last_tokens), dtype=torch.int32))
             t = t - 1
         self.kv.seq_len.copy_(t)
+        if self.four:
+            self.kv.entries.copy_(t)
         self.kv.status.zero_()
         self.step_dev.zero_()
+
+    def _evict(self):
+        """Holds the cache to its budget, if it has one."""
+        if self.bound is not None:
+            s2d2_kv4_evict(self.kv, *self.bound, stream=self.eng.stream)
 
     def step(self, prm: Params, n_accept: Optional[torch.Tensor] = None, n_commit: Optional[torch.Tensor] = None,
              advance: bool = True):
@@ -97,6 +136,7 @@ class Session:
         e.s2d2_verify(self.kv, self.st, N, B, prm, self.d, self.v)
         e.s2d2_accept(self.st, N, B, prm, self.d, self.v, self.a)
         e.s2d2_kv_append(self.kv, N, B, self.d, self.v, self.a.n_accept)
+        self._evict()
         if advance:
             e.s2d2_block_advance(self.kv, self.st, N, B, prm.step_dev)
 
@@ -115,6 +155,7 @@ class Session:
         e.s2d2_verify(self.kv, self.st, N, B, prm_r, self.d, self.v)
         e.s2d2_accept(self.st, N, B, prm_r, self.d, self.v, self.a)
         e.s2d2_kv_append(self.kv, N, B, self.d, self.v, self.a.n_accept)
+        self._evict()
         e.s2d2_commit_threshold(self.st, N, B, self._d_fallback)
         e.s2d2_block_advance(self.kv, self.st, N, B, prm.step_dev)
 
@@ -166,6 +207,7 @@ class Session:
                 if any((after[n] != mask).all() and max(0, int(P0[n] - S[n])) + B - max(0, min(B, int(S[n] - P0[n]))) > B
                        for n in range(N)):
                     e.s2d2_block_complete(self.kv, self.st, N, B, self.v, causal=1)
+            self._evict()
             n_acc, n_com = self.a.n_accept.cpu().numpy(), self.a.n_commit.cpu().numpy()
             for n in range(N):
                 if blocks_done[n] >= n_blocks:
