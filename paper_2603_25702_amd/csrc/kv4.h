@@ -56,6 +56,7 @@ struct Kv4Attn {
   float* lse;
   float scale_log2e;   // scores to base 2
   float *part_o, *part_ml;
+  int2* part_of;     // [N] of a sequence with several splits: its first item, its splits
   int32_t items;     // (sequence, split) pairs the grid holds
   int32_t per_item;  // workgroups of one: KV heads * groups of query tiles
   int32_t target;    // workgroups to aim for

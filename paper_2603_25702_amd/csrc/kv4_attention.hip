@@ -20,8 +20,8 @@ namespace s2d2 {
 //                 comes back transposed (ds_read_b64_tr_b16).  The rows of S^T are fed in an order that leaves the accumulators of a lane,
 //                 packed to half, as the operand P^T
 // A lane owns one query row (its column of S^T), so maximum, sum and scale need an exchange between two lanes only.  Scores are exponentiated
-// against a reference that lies 2^7 below the maximum it was taken from and follows the maximum when a weight would exceed 2^15: most
-// tiles rescale nothing, and half keeps 11 bits of a weight down to 2^-21 of the largest and 2^-32 of it below (with the maximum itself as the
+// against a reference that lies 2^7 below the maximum it was taken from and follows the maximum when the weights of a tile sum up to more than
+// 2^15: most tiles need no maximum and rescale nothing, and half keeps 11 bits of a weight down to 2^-21 of the largest and 2^-32 of it below (with the maximum itself as the
 // reference a million entries of 2^-24 each would lose a tenth of their weights).  Sums are in 32 bits.
 // Operands of more than 16 bits (fp32 models; queries in two planes) are split into planes of bf16, whose products are exact in 32 bits: 3
 // planes hold the 24 bits of a float.  Softmax weights are half (11 bits; off by at most 2^-12 of the weight), of fp32 models two half planes.
@@ -29,7 +29,8 @@ namespace s2d2 {
 // ---------------------------------------------------------------------------------------------
 static constexpr float LN2 = 0.69314718055994530942f;
 static constexpr float LOWEST = -3.402823466e38f;   // reference of a row that has seen nothing
-static constexpr float BELOW = 7.f, MOST = 15.f;    // a reference is taken this far below a maximum; scores exceed it by at most this (base 2)
+static constexpr float BELOW = 7.f;                 // a reference is taken this far below a maximum (base 2)
+static constexpr float MOST = 32768.f;              // and moves when the weights of a tile of keys sum up to more
 static constexpr int ATT_WAVES = 8;
 static constexpr int MIN_RUN = 32;                  // tiles of a split, at least: four a wavefront
 
@@ -122,22 +123,25 @@ __device__ __forceinline__ int wave_sum(int v) {
   for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
   return v;
 }
-// Tiles of a split: those of the whole batch over the workgroups that the launch aims for.
-__device__ __forceinline__ int run_length(const Kv4Attn& a, int lane) {
-  int total = 0;
-  for (int n0 = 0; n0 < a.N; n0 += 64) total += seq_tiles(a, n0 + lane).tiles;
-  const long long wanted = (long long)wave_sum(total) * a.per_item;
-  return max(MIN_RUN, (int)((wanted + a.target - 1) / a.target));
-}
 __device__ __forceinline__ int splits_of_seq(const SeqTiles& s, int run) { return s.rows == 0 ? 0 : max(1, (s.tiles + run - 1) / run); }
+
+// Tiles of a split.  The batch's tiles over the workgroups that are resident at once (target), less half a split a sequence, since the last split of each
+// is a partial one and a workgroup over the target would start when the others are done; at most half as much again as an equal share,
+// so that a long sequence among many short ones is still split.
+__device__ __forceinline__ int run_of(const Kv4Attn& a, int total) {
+  const long long wanted = 2ll * total * a.per_item, over = max(2ll * a.target - (long long)a.N * a.per_item, 4ll * a.target / 3);
+  return max(MIN_RUN, (int)((wanted + over - 1) / over));
+}
 
 // The sequence and split of item w; false: there is none.  All lanes of the wavefront, the same answer in each.
 struct Item { int n, z, splits, run; SeqTiles s; };
 __device__ __forceinline__ bool find_item(const Kv4Attn& a, int w, int lane, Item& it) {
-  it.run = run_length(a, lane);
+  SeqTiles s = seq_tiles(a, lane);
+  int total = s.tiles;
+  for (int n0 = 64; n0 < a.N; n0 += 64) total += seq_tiles(a, n0 + lane).tiles;
+  it.run = run_of(a, __builtin_amdgcn_readfirstlane(wave_sum(total)));
   int before = 0;
-  for (int n0 = 0; n0 < a.N; n0 += 64) {
-    const SeqTiles s = seq_tiles(a, n0 + lane);
+  for (int n0 = 0;;) {
     const int mine = splits_of_seq(s, it.run);
     int incl = mine;
 #pragma unroll
@@ -159,8 +163,10 @@ __device__ __forceinline__ bool find_item(const Kv4Attn& a, int w, int lane, Ite
       return true;
     }
     before += __builtin_amdgcn_readlane(incl, 63);
+    n0 += 64;
+    if (n0 >= a.N) return false;
+    s = seq_tiles(a, n0 + lane);
   }
-  return false;
 }
 
 // Half a key's codes (dimensions half * D / 2 and on) and the scale bytes of its groups
@@ -204,36 +210,48 @@ struct RowState {
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
   }
+  // The sum of a tile's weights says whether one of them may exceed the bound (an overflow sums to infinity; a row with a NaN stays one).
   __device__ __forceinline__ void weights(const f32x16_t& s, float scale, float (&p)[16]) {
-    float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+    float sum = 0.f;
+    auto form = [&]() __attribute__((always_inline)) {
+      sum = 0.f;
 #pragma unroll
-    for (int i = 3; i < 15; i += 2) mx = fmaxf(fmaxf(s[i], s[i + 1]), mx);
-    mx = fmaxf(mx, s[15]) * scale;
-    if (__ballot(mx > m + MOST)) {
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
+        sum += p[i];
+      }
+    };
+    form();
+    if (__ballot(sum > MOST)) {
+      float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+#pragma unroll
+      for (int i = 3; i < 15; i += 2) mx = fmaxf(fmaxf(s[i], s[i + 1]), mx);
+      mx = fmaxf(mx, s[15]) * scale;
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float to = mx > m + MOST ? mx - BELOW : m, f = __builtin_amdgcn_exp2f(m - to);
+      const float to = fmaxf(m, mx - BELOW), f = __builtin_amdgcn_exp2f(m - to);
       m = to;
       l *= f;
 #pragma unroll
       for (int t = 0; t < D / 32; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] *= f;
+      form();
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale, -m));
-      l += p[i];
-    }
+    l += sum;
   }
 };
 
 template <int D>
 static constexpr int V_LD = 2 * D + 32;   // bytes of a key's row of V in LDS: 16 lanes of a transposing read touch four rows, which then lie in different banks
 
+// QT == 1: queries in registers, the next tile's codes requested a tile ahead.  QT == 2: the conversion of K and V serves two query tiles;
+// their outputs take 128 registers, so the queries stay in LDS (one copy for the workgroup, in operand order) and the next codes are requested
+// into the registers of the converted ones.
 template <int D, int QM, int QT>
 __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4Attn a, int layer) {
   typedef typename Mode<QM>::T T;
   constexpr int QP = Mode<QM>::QP, PP = Mode<QM>::PP, WP = Mode<QM>::WP, WPP = Mode<QM>::WPP, NW = ATT_WAVES, DT = D / 32, DS = D / 16;
+  constexpr bool Q_LDS = QT > 1;
   extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
   const Kv4& kv = a.kv;
@@ -245,26 +263,56 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
   const SeqTiles& sq = it.s;
   const int nq = sq.rows * a.grp, q0 = qg * QT * 32;
   if (q0 >= nq) return;
-  const int t0 = it.z * it.run, t1 = min(sq.tiles, t0 + it.run);
+  const int t0 = it.z * it.run, t1 = min(sq.tiles, t0 + it.run), c1 = min(t1, sq.cached);
   const int tiles_q = min(QT, (nq - q0 + 31) / 32);
 
+  // ---- cached keys: lane (c, h) takes half h of key tile_key(c) of a tile ----
+  const int kperm = tile_key(c);
+  const int32_t* pt = kv.page_table + (size_t)it.n * kv.max_pages;
+  const uint8_t *kc = kv.kc + layer * kv.layer_entries * (D / 2), *vc = kv.vc + layer * kv.layer_entries * (D / 2);
+  const uint8_t *ks = kv.ks + layer * kv.layer_entries * (D / 32), *vs = kv.vs + layer * kv.layer_entries * (D / 32);
+  auto place_of = [&](int tile) __attribute__((always_inline)) { return min(tile * 32 + kperm, sq.S - 1); };
+  HalfRow<D> kn, vn;
+  int page_next = 0;
+  auto request_page = [&](int tile) __attribute__((always_inline)) { page_next = pt[kv.ps.div(place_of(tile))]; };
+  auto entry_of = [&](int tile) __attribute__((always_inline)) {
+    const int key = place_of(tile), p = kv.ps.div(key), page = max(0, min(page_next, kv.n_pages - 1));
+    return kv.at(page, kvh, key - p * kv.ps.d);
+  };
+  auto request = [&](int tile) __attribute__((always_inline)) {
+    const size_t at = entry_of(tile);
+    kn.load(kc, ks, at, h);
+    vn.load(vc, vs, at, h);
+  };
+  int tile = t0 + wave;
+  if (tile < c1) request_page(tile);
+
   // ---- queries: lane (c, h) has row c's dimensions h D / 2 + 8 ds .. + 7 for step ds ----
-  u32x4_t q[QT][DS][QP];
+  u32x4_t q[Q_LDS ? 1 : QT][Q_LDS ? 1 : DS][QP];
+  u32x4_t* s_q = (u32x4_t*)(s_mem + NW * 32 * V_LD<D>);   // [QT][DS][QP][64]
   int row[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int qi = min(q0 + t * 32 + c, nq - 1), r = a.group.div(qi);
     row[t] = sq.row0 + r;
     const T* p = (const T*)a.q + row[t] * a.q_ld + (size_t)(kvh * a.grp + qi - r * a.grp) * D + h * (D / 2);
+    if (Q_LDS) {
+      for (int ds = wave; ds < DS; ds += NW) {
+        u32x4_t x[QP];
+        load_planes<QP>(p + 8 * ds, a.q_lo, x);
 #pragma unroll
-    for (int ds = 0; ds < DS; ++ds) load_planes<QP>(p + 8 * ds, a.q_lo, q[t][ds]);
+        for (int e = 0; e < QP; ++e) s_q[((t * DS + ds) * QP + e) * 64 + lane] = x[e];
+      }
+    } else
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) load_planes<QP>(p + 8 * ds, a.q_lo, q[Q_LDS ? 0 : t][Q_LDS ? 0 : ds]);
   }
+  auto query = [&](int t, int ds, int e) __attribute__((always_inline)) { return Q_LDS ? s_q[((t * DS + ds) * QP + e) * 64 + lane] : q[Q_LDS ? 0 : t][Q_LDS ? 0 : ds][e]; };
   RowState<D> st[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) st[t].init();
 
   uint8_t* s_v = s_mem + (size_t)wave * 32 * V_LD<D>;   // this wavefront's tile of V
-  const int kperm = tile_key(c);
   const int g16 = lane >> 4, i16 = lane & 15;
   // transposing read: 16 lanes take 16 dimensions of 4 keys; lanes 0-31 keys 0-7, lanes 32-63 keys 8-15 of a step
   const uint8_t* s_tr = s_v + (8 * (g16 >> 1) + (i16 >> 2)) * V_LD<D> + ((g16 & 1) * 16 + (i16 & 3) * 4) * 2;
@@ -274,59 +322,64 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
     const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
     return u32x4_t{u.x, u.y, v.x, v.y};
   };
-
-  // ---- cached keys ----
-  const int32_t* pt = kv.page_table + (size_t)it.n * kv.max_pages;
-  const uint8_t *kc = kv.kc + layer * kv.layer_entries * (D / 2), *vc = kv.vc + layer * kv.layer_entries * (D / 2);
-  const uint8_t *ks = kv.ks + layer * kv.layer_entries * (D / 32), *vs = kv.vs + layer * kv.layer_entries * (D / 32);
-  const int c1 = min(t1, sq.cached);
-  auto place_of = [&](int tile) __attribute__((always_inline)) { return min(tile * 32 + kperm, sq.S - 1); };
-  HalfRow<D> kn, vn;
-  int page_next = 0;
-  auto request_page = [&](int tile) __attribute__((always_inline)) { page_next = pt[kv.ps.div(place_of(tile))]; };
-  auto request = [&](int tile) __attribute__((always_inline)) {
-    const int key = place_of(tile), p = kv.ps.div(key), page = max(0, min(page_next, kv.n_pages - 1));
-    const size_t at = kv.at(page, kvh, key - p * kv.ps.d);
-    kn.load(kc, ks, at, h);
-    vn.load(vc, vs, at, h);
+  u32x4_t* s_vrow = (u32x4_t*)(s_v + kperm * V_LD<D> + h * D);   // this lane's half row of V
+  auto lds_written = []() __attribute__((always_inline)) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   };
-  int tile = t0 + wave;
-  if (tile < c1) {
-    request_page(tile);
-    request(tile);
-    if (tile + NW < c1) request_page(tile + NW);
-  }
-  for (; tile < c1; tile += NW) {
-    const HalfRow<D> k = kn;
-    HalfRow<D> v = vn;
-    if (tile + NW < c1) {
-      request(tile + NW);
-      if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
+  auto lds_read = []() __attribute__((always_inline)) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+
+  // One tile of cached keys from k, v.  after_v(), after_k() run once V and K are converted.  Queries in LDS: the first half of a tile's operands is
+  // requested before V is converted, every further one when its predecessor's registers are free.
+  auto cached_tile = [&](int tile, const HalfRow<D>& k, HalfRow<D>& v, auto after_v, auto after_k) __attribute__((always_inline)) {
+    constexpr int AHEAD = Q_LDS ? (DS < 4 ? DS : 4) : 1;
+    u32x4_t qa[AHEAD][QT][QP];
+    if (Q_LDS) {
+#pragma unroll
+      for (int ds = 0; ds < AHEAD; ++ds)
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int p = 0; p < QP; ++p) qa[ds][t][p] = query(t, ds, p);
+      __builtin_amdgcn_sched_barrier(0);
     }
     const bool part = tile * 32 + 32 > sq.S;
     if (part && tile * 32 + kperm >= sq.S) v.clear();   // (what lies behind the entries may be anything)
 #pragma unroll
-    for (int i = 0; i < DS; ++i) *(u32x4_t*)(s_v + kperm * V_LD<D> + h * D + 16 * i) = codes_f16(v.w[i], v.scale(i));
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    for (int i = 0; i < DS; ++i) s_vrow[i] = codes_f16(v.w[i], v.scale(i));
+    lds_written();
+    after_v();
+    f32x16_t s[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) {
+      const u32x4_t kf = codes_bf16(k.w[ds], k.scale(ds));
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int p = 0; p < QP; ++p) {
+          s[t] = mfma_bf16(kf, Q_LDS ? qa[ds % AHEAD][t][p] : query(t, ds, p), s[t]);
+          if (Q_LDS && ds + AHEAD < DS) qa[ds % AHEAD][t][p] = query(t, ds + AHEAD, p);
+        }
+      if (Q_LDS) __builtin_amdgcn_sched_barrier(0);
+    }
+    after_k();
     u32x4_t pw[QT][2][PP];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      f32x16_t s;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int ds = 0; ds < DS; ++ds) {
-        const u32x4_t kf = codes_bf16(k.w[ds], k.scale(ds));
-#pragma unroll
-        for (int p = 0; p < QP; ++p) s = mfma_bf16(kf, q[t][ds][p], s);
-      }
       if (part) {
+        const int left = sq.S - tile * 32 - 8 * h;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = tile * 32 + 16 * (i >> 3) + 8 * h + (i & 7) < sq.S ? s[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) s[t][i] = 16 * (i >> 3) + (i & 7) < left ? s[t][i] : -INFINITY;
       }
       float p[16];
-      st[t].weights(s, a.scale_log2e, p);
+      st[t].weights(s[t], a.scale_log2e, p);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -352,53 +405,88 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
 #pragma unroll
           for (int e = 0; e < PP; ++e) st[t].o[dt] = mfma_f16(vf, pw[t][j][e], st[t].o[dt]);
       }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    lds_read();
+  };
+  if (tile < c1) {
+    request(tile);
+    if (tile + NW < c1) request_page(tile + NW);
+  }
+  if (Q_LDS) __syncthreads();
+  if (Q_LDS) {
+    size_t at = 0;
+    for (; tile < c1; tile += NW)
+      cached_tile(tile, kn, vn, [&]() __attribute__((always_inline)) {
+        if (tile + NW < c1) {
+          at = entry_of(tile + NW);
+          vn.load(vc, vs, at, h);
+          if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
+        }
+      }, [&]() __attribute__((always_inline)) {
+        if (tile + NW < c1) kn.load(kc, ks, at, h);
+      });
+  } else {
+    for (; tile < c1; tile += NW) {
+      const HalfRow<D> k = kn;
+      HalfRow<D> v = vn;
+      if (tile + NW < c1) {
+        request(tile + NW);
+        if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
+      }
+      cached_tile(tile, k, v, []() {}, []() {});
+    }
   }
 
-  // ---- the window's own keys: plane by plane ----
+  // ---- the window's own keys: V plane by plane through LDS ----
   for (; tile < t1; tile += NW) {
     const int base = (tile - sq.cached) * 32, key = base + kperm;
     const bool there = key < sq.rows;
     const int64_t at = (int64_t)(sq.row0 + min(key, sq.rows - 1)) * a.kv_ld + kvh * D + h * (D / 2);
-    u32x4_t kf[DS][WP], vf[DS][WP];
     bool bad = false;   // a value of this key that is not finite: the rows that see it become NaN, the others must not
 #pragma unroll
     for (int ds = 0; ds < DS; ++ds) {
-      load_planes<WP>((const T*)a.k + at + 8 * ds, 0, kf[ds]);
-      load_planes<WP>((const T*)a.v + at + 8 * ds, 0, vf[ds]);
+      u32x4_t v[WP];
+      load_planes<WP>((const T*)a.v + at + 8 * ds, 0, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= (vf[ds][0][i] & 0x7f80u) == 0x7f80u || (vf[ds][0][i] & 0x7f800000u) == 0x7f800000u;
+      for (int i = 0; i < 4; ++i) bad |= (v[0][i] & 0x7f80u) == 0x7f80u || (v[0][i] & 0x7f800000u) == 0x7f800000u;
+      s_vrow[ds] = there ? v[0] : u32x4_t{0, 0, 0, 0};
     }
     bad |= (bool)__shfl_xor((int)bad, 32, 64);
     const unsigned long long bad_at = __ballot(there && bad);   // bit c: key tile_key(c)
-#pragma unroll
-    for (int ds = 0; ds < DS; ++ds)
-#pragma unroll
-      for (int e = 0; e < WP; ++e)
-        if (!there || bad) vf[ds][e] = u32x4_t{0, 0, 0, 0};
-    u32x4_t pw[QT][2][WPP];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      f32x16_t s;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    if (bad_at) {
 #pragma unroll
       for (int ds = 0; ds < DS; ++ds)
+        if (bad) s_vrow[ds] = u32x4_t{0, 0, 0, 0};
+    }
+    lds_written();
+    f32x16_t s[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) {
+      u32x4_t kf[WP];
+      load_planes<WP>((const T*)a.k + at + 8 * ds, 0, kf);
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int e = 0; e < WP; ++e)
 #pragma unroll
           for (int p = 0; p < QP; ++p)
-            if (e + p < (QP > WP ? QP : WP)) s = mfma_bf16(kf[ds][e], q[t][ds][p], s);
+            if (e + p < (QP > WP ? QP : WP)) s[t] = mfma_bf16(kf[e], query(t, ds, p), s[t]);
+    }
+    u32x4_t pw[QT][2][WPP];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
       const int lo = a.lo ? a.lo[row[t]] : sq.row0, hi = a.hi ? a.hi[row[t]] : row[t] + 1;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int rr = 8 * (i >> 2) + 4 * h + (i & 3), k = base + tile_key(rr), r = sq.row0 + k;
         const bool seen = k < sq.rows && ((r >= lo && r < hi) || r == row[t]);
-        s[i] = !seen ? -INFINITY : (bad_at >> rr) & 1 ? NAN : s[i];
+        s[t][i] = !seen ? -INFINITY : (bad_at >> rr) & 1 ? NAN : s[t][i];
       }
       float p[16];
-      st[t].weights(s, a.scale_log2e, p);
+      st[t].weights(s[t], a.scale_log2e, p);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float x[8] = {p[8 * j], p[8 * j + 1], p[8 * j + 2], p[8 * j + 3], p[8 * j + 4], p[8 * j + 5], p[8 * j + 6], p[8 * j + 7]};
@@ -407,10 +495,15 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
     }
 #pragma unroll
     for (int e = 0; e < WP; ++e) {
+      if (e > 0) {
 #pragma unroll
-      for (int ds = 0; ds < DS; ++ds) *(u32x4_t*)(s_v + kperm * V_LD<D> + h * D + 16 * ds) = vf[ds][e];
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+        for (int ds = 0; ds < DS; ++ds) {
+          u32x4_t v[WP];
+          load_planes<WP>((const T*)a.v + at + 8 * ds, 0, v);
+          s_vrow[ds] = there && !bad ? v[e] : u32x4_t{0, 0, 0, 0};
+        }
+        lds_written();
+      }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -422,8 +515,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
             for (int p = 0; p < WPP; ++p)
               if (e + p < WPP) st[t].o[dt] = mfma_bf16(vo, pw[t][j][p], st[t].o[dt]);
         }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+      lds_read();
     }
   }
 
@@ -479,10 +571,11 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
             }
           if (a.lse && h == 0) a.lse[(size_t)row[t] * a.Hq + head] = st[t].l == 0.f ? -INFINITY : (st[t].m + __builtin_amdgcn_logf(st[t].l)) * LN2;
         }
-      } else {
-        // partial output in the accumulators' order, then maxima and sums
+      } else if (qi < nq) {
+        // partial output in the accumulators' order, then maxima and sums; the first split says where the sequence's are
         const size_t at = ((size_t)w * groups + qg) * QT + t;
         float4* po = (float4*)(a.part_o + at * 32 * D);
+        if (t == 0 && qg == 0 && kvh == 0 && it.z == 0 && lane == 0) a.part_of[it.n] = make_int2(w / kv.H, it.splits);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -494,42 +587,55 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
   }
 }
 
-// The splits of a (sequence, KV head, query tile) into its rows, in the order of the splits.
+// The splits of a (sequence, KV head, query tile) into its rows, in the order of the splits; a workgroup has 32 dimensions, a thread four of a
+// row.  Sequences of one split are done; Z: splits of a sequence, at most `most`.
 template <int D, int QM>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int tiles, int per_wg) {
   const Kv4& kv = a.kv;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int qt = blockIdx.x % tiles, kvh = (blockIdx.x / tiles) % kv.H, n = blockIdx.x / tiles / kv.H;
-  const int run = run_length(a, lane);
-  int first = 0;
-  for (int n0 = 0; n0 < n; n0 += 64) first += n0 + lane < n ? splits_of_seq(seq_tiles(a, n0 + lane), run) : 0;
-  first = wave_sum(first);
+  const int tid = threadIdx.x, c = tid & 31, h = (tid >> 5) & 1, g = tid >> 6;
+  const int dt = blockIdx.x % (D / 32), b = blockIdx.x / (D / 32), qt = b % tiles, kvh = (b / tiles) % kv.H, n = b / tiles / kv.H;
+  const int2 of = a.part_of[n];     // (of a sequence with one split, or none: what the scratch held)
   const SeqTiles sq = seq_tiles(a, n);
-  const int Z = splits_of_seq(sq, run), nq = sq.rows * a.grp;
-  if (Z < 2 || qt * 32 >= nq) return;
-  const int groups = a.per_item / kv.H, qg = qt / per_wg, t = qt % per_wg;
-  auto part = [&](int z) __attribute__((always_inline)) { return ((size_t)((first + z) * kv.H + kvh) * groups + qg) * per_wg + t; };
-  // element e (four outputs): lane 32 h + c, group e / 64 = dt * 4 + i
-  for (int e = tid; e < 8 * D; e += 256) {
-    const int c = e & 31, h = (e >> 5) & 1, g = e >> 6;
-    float m = LOWEST, l = 0.f;
-    for (int z = 0; z < Z; ++z) m = fmaxf(m, a.part_ml[part(z) * 64 + c]);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int z = 0; z < Z; ++z) {
-      const size_t at = part(z);
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[at * 64 + c] - m);
-      const float4 v = ((const float4*)(a.part_o + at * 32 * D))[e];
-      l += f * a.part_ml[at * 64 + 32 + c];
-      o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+  const int nq = sq.rows * a.grp, qi = qt * 32 + c;
+  if (qt * 32 >= nq || sq.tiles <= MIN_RUN) return;
+  int total = 0;
+  for (int n0 = tid & 63; n0 < a.N; n0 += 64) total += seq_tiles(a, n0).tiles;
+  if (sq.tiles <= run_of(a, __builtin_amdgcn_readfirstlane(wave_sum(total)))) return;
+  if (qi >= nq) return;
+  const int Z = of.y, groups = a.per_item / kv.H;
+  const size_t step = (size_t)kv.H * groups * per_wg, at0 = (((size_t)of.x * kv.H + kvh) * groups + qt / per_wg) * per_wg + qt % per_wg;
+  const float* ml = a.part_ml + at0 * 64 + c;
+  const float4* po = (const float4*)(a.part_o + at0 * 32 * D) + (dt * 4 + g) * 64 + 32 * h + c;
+  float m = LOWEST, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int AHEAD = 8;   // splits in flight
+  for (int z0 = 0; z0 < Z; z0 += AHEAD) {
+    float mz[AHEAD], lz[AHEAD];
+    float4 v[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int z = min(z0 + k, Z - 1);
+      mz[k] = ml[z * step * 64];
+      lz[k] = ml[z * step * 64 + 32];
+      v[k] = po[z * step * 8 * D];
     }
-    const int qi = qt * 32 + c;
-    if (qi >= nq) continue;
-    const int r = a.group.div(qi), row = sq.row0 + r, head = kvh * a.grp + qi - r * a.grp, d = head * D + (g >> 2) * 32 + 8 * (g & 3) + 4 * h;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (QM == Q_F32) *(float4*)((float*)a.out + row * a.o_ld + d) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    else act_put4((bf16_t*)a.out, a.o_lo, row, d, (int)a.o_ld, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    if (a.lse && g == 0 && h == 0) a.lse[(size_t)row * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+    float to = m;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) to = fmaxf(to, mz[k]);
+    const float f0 = __builtin_amdgcn_exp2f(m - to);
+    l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+    m = to;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float f = z0 + k < Z ? __builtin_amdgcn_exp2f(mz[k] - m) : 0.f;
+      if (z0 + k < Z) { l += f * lz[k]; o.x += f * v[k].x; o.y += f * v[k].y; o.z += f * v[k].z; o.w += f * v[k].w; }
+    }
   }
+  const int r = a.group.div(qi), row = sq.row0 + r, head = kvh * a.grp + qi - r * a.grp, d = head * D + dt * 32 + 8 * g + 4 * h;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (QM == Q_F32) *(float4*)((float*)a.out + row * a.o_ld + d) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  else act_put4((bf16_t*)a.out, a.o_lo, row, d, (int)a.o_ld, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  if (a.lse && dt == 0 && g == 0 && h == 0) a.lse[(size_t)row * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -589,7 +695,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_weigh_kernel(const Kv4Attn
 // ---------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------
-static constexpr int TARGET = 512;   // workgroups of a launch: two a compute unit
+static constexpr int TARGET = 256;   // workgroups that are resident at once: one a compute unit (eight wavefronts of up to 256 registers)
 
 // Query tiles per workgroup: two share the conversion of K and V; one where there is no second, and where two would not leave registers.
 static int tiles_per_wg(int D, int dtype, int planes, int q_tiles) { return D <= 128 && dtype == S2D2_BF16 && planes == 1 && q_tiles >= 2 ? 2 : 1; }
@@ -613,17 +719,20 @@ size_t kv4_attention_bytes(const Kv4& kv, int N, int T, int Hq) {
   const AttnShape s = shape_of(kv, S2D2_BF16, 1, N, T, Hq, true);
   if (s.most < 2) return 0;
   const size_t slots = 2 * TARGET + ((size_t)(N + 1) * kv.H + 8) * (s.q_tiles + 1);
-  return (slots * (32 * kv.D + 64) * sizeof(float) + 255) & ~(size_t)255;
+  return ((slots * (32 * kv.D + 64) + 2 * N) * sizeof(float) + 255) & ~(size_t)255;
 }
 
-template <int D>
-static constexpr size_t attn_lds() { return std::max((size_t)ATT_WAVES * 32 * V_LD<D>, (size_t)(ATT_WAVES / 2) * (32 * D + 64) * sizeof(float)); }
+// Tiles of V and the queries, and after them the wavefronts' states.
+template <int D, int QT>
+static constexpr size_t attn_lds() {
+  return std::max((size_t)ATT_WAVES * 32 * V_LD<D> + (QT > 1 ? (size_t)QT * 32 * D * 2 : 0), (size_t)(ATT_WAVES / 2) * (32 * D + 64) * sizeof(float));
+}
 
 template <int D, int QM, int QT>
 static void launch_attn(hipStream_t st, const Kv4Attn& a, int layer, const AttnShape& s) {
   const int wgs = (a.items * a.kv.H + 7) / 8 * 8 * s.groups;
-  S2D2_LAUNCH((kv4_attention_kernel<D, QM, QT>), dim3(wgs), dim3(64 * ATT_WAVES), attn_lds<D>(), st, a, layer);
-  if (s.most > 1) S2D2_LAUNCH((kv4_merge_kernel<D, QM>), dim3(a.N * a.kv.H * s.q_tiles), dim3(256), 0, st, a, s.q_tiles, s.per_wg);
+  S2D2_LAUNCH((kv4_attention_kernel<D, QM, QT>), dim3(wgs), dim3(64 * ATT_WAVES), (attn_lds<D, QT>()), st, a, layer);
+  if (s.most > 1) S2D2_LAUNCH((kv4_merge_kernel<D, QM>), dim3(a.N * a.kv.H * s.q_tiles * (D / 32)), dim3(256), 0, st, a, s.q_tiles, s.per_wg);
 }
 
 template <typename F>
@@ -642,6 +751,7 @@ void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int
   const size_t slots = (size_t)((s.items * a.kv.H + 7) / 8 * 8) * s.groups * s.per_wg;
   a.part_o = (float*)scratch;
   a.part_ml = a.part_o + slots * 32 * a.kv.D;
+  a.part_of = (int2*)(a.part_ml + slots * 64);
   by_head_dim(a.kv.D, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     if (dtype == S2D2_F32) launch_attn<D, Q_F32, 1>(st, a, layer, s);
@@ -673,10 +783,10 @@ int kv4_attention_init() {
   for (int D : {32, 64, 128, 256})
     by_head_dim(D, [&](auto dim) {
       constexpr int D = decltype(dim)::value;
-      limit((const void*)kv4_attention_kernel<D, Q_BF16, 1>, attn_lds<D>());
-      limit((const void*)kv4_attention_kernel<D, Q_BF16X2, 1>, attn_lds<D>());
-      limit((const void*)kv4_attention_kernel<D, Q_F32, 1>, attn_lds<D>());
-      if (D <= 128) limit((const void*)kv4_attention_kernel<(D <= 128 ? D : 128), Q_BF16, 2>, attn_lds<(D <= 128 ? D : 128)>());
+      limit((const void*)kv4_attention_kernel<D, Q_BF16, 1>, attn_lds<D, 1>());
+      limit((const void*)kv4_attention_kernel<D, Q_BF16X2, 1>, attn_lds<D, 1>());
+      limit((const void*)kv4_attention_kernel<D, Q_F32, 1>, attn_lds<D, 1>());
+      if (D <= 128) limit((const void*)kv4_attention_kernel<(D <= 128 ? D : 128), Q_BF16, 2>, attn_lds<(D <= 128 ? D : 128), 2>());
     });
   return e == hipSuccess ? 0 : -1;
 }
