@@ -101,8 +101,14 @@ int32_t s2d2_kv4_weigh(void* stream, const s2d2_kv4_view* kv, int32_t layer, con
  * first `sink` positions (position < sink) and of the last `recent` (position >= seq_len[n] - recent), then those of the largest mass; ties: the
  * lower entry first; a NaN counts as less than any other mass.  The i-th entry below `budget` that goes is replaced by the i-th one from `budget` on that stays
  * (codes, scales, mass and position as they are); all others stay where they are.  entries[n] becomes budget.  Needs mass and position;
- * budget >= 1, slack >= 0, sink + recent <= budget.  N <= 1024. */
-int32_t s2d2_kv4_evict(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t budget, int32_t slack, int32_t sink, int32_t recent);
+ * budget >= 1, slack >= 0, sink + recent <= budget.  N <= 1024.  scratch: device, 4-byte aligned, s2d2_kv4_evict_bytes() or more; its contents do not
+ * matter and nothing is kept in it.  Calls that run at the same time need a scratch (and a cache) each. */
+int32_t s2d2_kv4_evict(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t budget, int32_t slack, int32_t sink, int32_t recent, void* scratch,
+                       size_t scratch_bytes);
+
+/* Bytes of scratch that s2d2_kv4_evict needs for N sequences of this cache, whatever the budget (4 bytes for every place of a list and 4 for the
+ * list); negative S2D2_E* on bad arguments. */
+int64_t s2d2_kv4_evict_bytes(const s2d2_kv4_view* kv, int32_t N);
 
 /* From this call on the calls of s2d2.h on `ctx` that take an s2d2_kv_view keep the prefix in this cache (NULL: in the view's own pages again).
  * Their views then have to describe it: k_pages = k_codes, v_pages = v_codes, the same page_table, seq_len, n_pages, page_size and

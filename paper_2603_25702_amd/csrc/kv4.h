@@ -60,6 +60,7 @@ struct Kv4Attn {
   int32_t items;     // (sequence, split) pairs the grid holds
   int32_t per_item;  // workgroups of one: KV heads * groups of query tiles
   int32_t target;    // workgroups to aim for
+  int32_t min_run;   // tiles of a split, at least
   Divisor group;     // by query heads per KV head
 };
 
@@ -81,6 +82,7 @@ struct Kv4Rows {
 };
 void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv4Rows& r, const void* k, const void* v, int64_t layer_stride, int64_t row_stride);
 void launch_kv4_read(hipStream_t st, int dtype, const Kv4& kv, int N, int T, const int32_t* first, void* k, void* v);
-void launch_kv4_evict(hipStream_t st, const Kv4& kv, int N, int budget, int slack, int sink, int recent);
+void launch_kv4_evict(hipStream_t st, const Kv4& kv, int N, int budget, int slack, int sink, int recent, void* scratch);
+size_t kv4_evict_bytes(const Kv4& kv, int N);
 
 }  // namespace s2d2

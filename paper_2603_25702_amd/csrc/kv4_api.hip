@@ -138,13 +138,23 @@ int32_t s2d2_kv4_weigh(void* stream, const s2d2_kv4_view* kv, int32_t layer, con
   return check_launch("s2d2_kv4_weigh");
 }
 
-int32_t s2d2_kv4_evict(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t budget, int32_t slack, int32_t sink, int32_t recent) {
+int64_t s2d2_kv4_evict_bytes(const s2d2_kv4_view* kv, int32_t N) {
+  int32_t rc;
+  if ((rc = check_kv4(kv)) || (rc = check_batch(N, 1, 1))) return rc;
+  return (int64_t)kv4_evict_bytes(kv4_of(kv), N);
+}
+
+int32_t s2d2_kv4_evict(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t budget, int32_t slack, int32_t sink, int32_t recent, void* scratch,
+                       size_t scratch_bytes) {
   int32_t rc;
   if ((rc = check_kv4(kv)) || (rc = check_batch(N, 1, 1))) return rc;
   if (!kv->mass || !kv->position) return fail(S2D2_EINVAL, "eviction needs the cache's mass and position");
   if (budget < 1 || slack < 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > budget) return fail(S2D2_EINVAL, "budget=%d must be positive, slack=%d, sink=%d and recent=%d non-negative, sink + recent at most budget", budget, slack, sink, recent);
+  const size_t need = kv4_evict_bytes(kv4_of(kv), N);
+  if (scratch_bytes < need) return fail(S2D2_ENOSPC, "scratch has %zu bytes, %zu needed", scratch_bytes, need);
+  if (!scratch || ((uintptr_t)scratch & 3)) return fail(S2D2_EINVAL, "scratch is NULL or not 4-byte aligned");
   if ((rc = kv4_ready())) return rc;
-  launch_kv4_evict((hipStream_t)stream, kv4_of(kv), N, budget, slack, sink, recent);
+  launch_kv4_evict((hipStream_t)stream, kv4_of(kv), N, budget, slack, sink, recent, scratch);
   return check_launch("s2d2_kv4_evict");
 }
 

@@ -130,7 +130,7 @@ __device__ __forceinline__ int splits_of_seq(const SeqTiles& s, int run) { retur
 // so that a long sequence among many short ones is still split.
 __device__ __forceinline__ int run_of(const Kv4Attn& a, int total) {
   const long long wanted = 2ll * total * a.per_item, over = max(2ll * a.target - (long long)a.N * a.per_item, 4ll * a.target / 3);
-  return max(MIN_RUN, (int)((wanted + over - 1) / over));
+  return max(a.min_run, (int)((wanted + over - 1) / over));
 }
 
 // The sequence and split of item w; false: there is none.  All lanes of the wavefront, the same answer in each.
@@ -597,7 +597,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int til
   const int2 of = a.part_of[n];     // (of a sequence with one split, or none: what the scratch held)
   const SeqTiles sq = seq_tiles(a, n);
   const int nq = sq.rows * a.grp, qi = qt * 32 + c;
-  if (qt * 32 >= nq || sq.tiles <= MIN_RUN) return;
+  if (qt * 32 >= nq || sq.tiles <= a.min_run) return;
   int total = 0;
   for (int n0 = tid & 63; n0 < a.N; n0 += 64) total += seq_tiles(a, n0).tiles;
   if (sq.tiles <= run_of(a, __builtin_amdgcn_readfirstlane(wave_sum(total)))) return;
@@ -640,61 +640,122 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int til
 
 // ---------------------------------------------------------------------------------------------
 // kv4_weigh_kernel: the weights that a sequence's rows give its entries.  A workgroup has one sequence, one KV head and a run of key tiles, a
-// wavefront every NW-th tile.  Scores are computed as S = Q K^T, so that a lane owns a key and the sum over rows stays in it; the sums of a tile
-// over all query tiles are added to the mass once, by one lane a key, in a fixed order.
+// wavefront every fourth pair of them.  Scores are computed as S = Q K^T, so that a lane owns a key and the sum over rows stays in it; the queries
+// lie in LDS in operand order, up to QC tiles of 32 rows at a time, each read for two tiles of keys.  The sums of a pair over these rows are
+// added to the mass by one lane a key, tile of rows after tile of rows: a fixed order.
+// Bound: the exponentials (16 cycles each, with a multiply-add and an add 24 for 64 scores); the matrix instructions of a tile take 256 cycles beside
+// 384 of these.
 // ---------------------------------------------------------------------------------------------
+static constexpr int WEIGH_WAVES = 4;
 template <int D, int QM>
-__global__ __launch_bounds__(64 * ATT_WAVES) void kv4_weigh_kernel(const Kv4Attn a, int layer) {
+static constexpr int QC = D * Mode<QM>::QP <= 384 ? 4 : 2;
+template <int D, int QM>
+static constexpr size_t weigh_lds() { return (size_t)QC<D, QM> * (32 * D * 2 * Mode<QM>::QP + 33 * sizeof(float)); }
+
+template <int D, int QM>
+__global__ __launch_bounds__(64 * WEIGH_WAVES, D <= 128 ? 3 : 2) void kv4_weigh_kernel(const Kv4Attn a, int layer) {
   typedef typename Mode<QM>::T T;
-  constexpr int QP = Mode<QM>::QP, NW = ATT_WAVES, DS = D / 16;
+  constexpr int QP = Mode<QM>::QP, NW = WEIGH_WAVES, DS = D / 16, C = QC<D, QM>;
+  extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
+  u32x4_t* s_q = (u32x4_t*)s_mem;                       // [C][DS][QP][64]
+  float* s_ref = (float*)(s_q + C * DS * QP * 64);      // [C][32] minus a row's lse to base 2; -inf: the row adds nothing
+  int* s_some = (int*)(s_ref + C * 32);                 // [C] whether there is such a row
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
   const Kv4& kv = a.kv;
   const int kvh = blockIdx.x % kv.H;
   Item it;
   if (!find_item(a, blockIdx.x / kv.H, lane, it)) return;
   const SeqTiles& sq = it.s;
-  const int nq = sq.rows * a.grp, t1 = min(sq.cached, (it.z + 1) * it.run);
+  const int nq = sq.rows * a.grp, t0 = it.z * it.run, t1 = min(sq.cached, t0 + it.run);
   const int32_t* pt = kv.page_table + (size_t)it.n * kv.max_pages;
-  const size_t layer0 = layer * kv.layer_entries;
-  for (int tile = it.z * it.run + wave; tile < t1; tile += NW) {
-    const int key = tile * 32 + c, k0 = min(key, sq.S - 1), p = kv.ps.div(k0), page = pt[p];
-    const size_t at = layer0 + kv.at(max(0, min(page, kv.n_pages - 1)), kvh, k0 - p * kv.ps.d);
-    HalfRow<D> k;
-    k.load(kv.kc, kv.ks, at, h);
-    u32x4_t kf[DS];
+  const uint8_t *kc = kv.kc + layer * kv.layer_entries * (D / 2), *ks = kv.ks + layer * kv.layer_entries * (D / 32);
+  HalfRow<D> next[2];
+  auto entry = [&](int key, int& page) __attribute__((always_inline)) {
+    const int k = min(key, sq.S - 1), p = kv.ps.div(k);
+    page = pt[p];
+    return kv.at(max(0, min(page, kv.n_pages - 1)), kvh, k - p * kv.ps.d);
+  };
+  auto request = [&](int tile) __attribute__((always_inline)) {
+    int page;
 #pragma unroll
-    for (int ds = 0; ds < DS; ++ds) kf[ds] = codes_bf16(k.w[ds], k.scale(ds));
-    float sum = 0.f;
-    for (int q0 = 0; q0 < nq; q0 += 32) {
-      const int qi = min(q0 + c, nq - 1), r = a.group.div(qi);
-      const T* qp = (const T*)a.q + (sq.row0 + r) * a.q_ld + (size_t)(kvh * a.grp + qi - r * a.grp) * D + h * (D / 2);
-      // of row c: its lse to base 2, or what makes every weight 0
-      const float e = a.lse[(size_t)(sq.row0 + r) * a.Hq + kvh * a.grp + qi - r * a.grp];
-      const float mine = q0 + c >= nq || e == -INFINITY ? INFINITY : e * (1.f / LN2);
-      f32x16_t s;
+    for (int x = 0; x < 2; ++x) next[x].load(kc, ks, entry((tile + x) * 32 + c, page), h);   // (a tile behind the last: entries that are there)
+  };
+  for (int q0 = 0; q0 < nq; q0 += 32 * C) {
+    const int tiles = min(C, (nq - q0 + 31) / 32);
+    if (q0) __syncthreads();
+    for (int i = wave; i < tiles * DS; i += NW) {
+      const int t = i / DS, ds = i % DS, qi = min(q0 + t * 32 + c, nq - 1), r = a.group.div(qi), head = kvh * a.grp + qi - r * a.grp;
+      u32x4_t x[QP];
+      load_planes<QP>((const T*)a.q + (sq.row0 + r) * a.q_ld + (size_t)head * D + h * (D / 2) + 8 * ds, a.q_lo, x);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int ds = 0; ds < DS; ++ds) {
-        u32x4_t qf[QP];
-        load_planes<QP>(qp + 8 * ds, a.q_lo, qf);
-#pragma unroll
-        for (int e2 = 0; e2 < QP; ++e2) s = mfma_bf16(qf[e2], kf[ds], s);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float ref = __shfl(mine, 8 * (i >> 2) + 4 * h + (i & 3), 64);
-        sum += ref == INFINITY ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2e, -ref));
+      for (int e = 0; e < QP; ++e) s_q[(i * QP + e) * 64 + lane] = x[e];
+      if (ds == 0) {
+        const float lse = a.lse[(size_t)(sq.row0 + r) * a.Hq + head];
+        const float ref = q0 + t * 32 + c >= nq || lse == -INFINITY ? -INFINITY : -lse * (1.f / LN2);
+        if (h == 0) s_ref[t * 32 + c] = ref;
+        const bool some = __ballot(ref == -INFINITY) != 0;
+        if (lane == 0) s_some[t] = some;
       }
     }
-    sum += __shfl_xor(sum, 32, 64);
-    if (h == 0 && key < sq.S && page >= 0 && page < kv.n_pages) kv.mass[at] += sum;
+    int tile = t0 + 2 * wave;
+    if (tile < t1) request(tile);
+    __syncthreads();
+    for (; tile < t1; tile += 2 * NW) {
+      u32x4_t kf[2][DS];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds) kf[x][ds] = codes_bf16(next[x].w[ds], next[x].scale(ds));
+      if (tile + 2 * NW < t1) request(tile + 2 * NW);
+      float sum[2] = {0.f, 0.f};
+      for (int t = 0; t < tiles; ++t) {
+        f32x16_t s[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+          for (int e = 0; e < QP; ++e) {
+            const u32x4_t qf = s_q[((t * DS + ds) * QP + e) * 64 + lane];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) s[x] = mfma_bf16(qf, kf[x][ds], s[x]);
+          }
+        float ref[16];   // of rows 8 (i / 4) + 4 h + i % 4
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 v = *(const float4*)(s_ref + t * 32 + 8 * i + 4 * h);
+          ref[4 * i] = v.x; ref[4 * i + 1] = v.y; ref[4 * i + 2] = v.z; ref[4 * i + 3] = v.w;
+        }
+        const bool some = __builtin_amdgcn_readfirstlane(s_some[t]);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][i], a.scale_log2e, ref[i]));
+          if (some)   // (a key that reads as NaN has no weight from rows that add nothing)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = ref[i] == -INFINITY ? 0.f : p[i];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[x] += p[i];
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) sum[x] += __shfl_xor(sum[x], 32, 64);
+      // lane (c, h): key c of the pair's tile h
+      const int key = (tile + h) * 32 + c;
+      int page;
+      const size_t at = layer * kv.layer_entries + entry(key, page);
+      if (tile + h < t1 && key < sq.S && page >= 0 && page < kv.n_pages) kv.mass[at] += h ? sum[1] : sum[0];
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------------------------
+static constexpr int WEIGH_TARGET = 768, WEIGH_MIN_RUN = 16;   // three workgroups a compute unit (four wavefronts of up to 168 registers); two pairs of tiles a wavefront
 static constexpr int TARGET = 256;   // workgroups that are resident at once: one a compute unit (eight wavefronts of up to 256 registers)
 
 // Query tiles per workgroup: two share the conversion of K and V; one where there is no second, and where two would not leave registers.
@@ -748,6 +809,7 @@ void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int
   a.items = s.items;
   a.per_item = a.kv.H * s.groups;
   a.target = TARGET;
+  a.min_run = MIN_RUN;
   const size_t slots = (size_t)((s.items * a.kv.H + 7) / 8 * 8) * s.groups * s.per_wg;
   a.part_o = (float*)scratch;
   a.part_ml = a.part_o + slots * 32 * a.kv.D;
@@ -763,16 +825,17 @@ void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int
 
 void launch_kv4_weigh(hipStream_t st, int dtype, int planes, Kv4Attn& a, int layer) {
   a.k = a.v = nullptr;
-  const AttnShape s = shape_of(a.kv, dtype, planes, a.N, a.T, a.Hq, false);
   a.per_item = a.kv.H;
-  a.target = TARGET;
-  a.items = (int)std::min<long long>((long long)a.N * s.most, (TARGET + a.kv.H - 1) / a.kv.H + (long long)a.N);
+  a.target = WEIGH_TARGET;
+  a.min_run = WEIGH_MIN_RUN;
+  const int most = std::max(1, ((a.kv.cap + 31) / 32 + WEIGH_MIN_RUN - 1) / WEIGH_MIN_RUN);
+  a.items = (int)std::min<long long>((long long)a.N * most, (WEIGH_TARGET + a.kv.H - 1) / a.kv.H + (long long)a.N);
   by_head_dim(a.kv.D, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    const dim3 grid(a.items * a.kv.H), wg(64 * ATT_WAVES);
-    if (dtype == S2D2_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32>), grid, wg, 0, st, a, layer);
-    else if (planes == 2) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16X2>), grid, wg, 0, st, a, layer);
-    else S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16>), grid, wg, 0, st, a, layer);
+    const dim3 grid(a.items * a.kv.H), wg(64 * WEIGH_WAVES);
+    if (dtype == S2D2_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32>), grid, wg, (weigh_lds<D, Q_F32>()), st, a, layer);
+    else if (planes == 2) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16X2>), grid, wg, (weigh_lds<D, Q_BF16X2>()), st, a, layer);
+    else S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16>), grid, wg, (weigh_lds<D, Q_BF16>()), st, a, layer);
   });
 }
 
@@ -786,6 +849,9 @@ int kv4_attention_init() {
       limit((const void*)kv4_attention_kernel<D, Q_BF16, 1>, attn_lds<D, 1>());
       limit((const void*)kv4_attention_kernel<D, Q_BF16X2, 1>, attn_lds<D, 1>());
       limit((const void*)kv4_attention_kernel<D, Q_F32, 1>, attn_lds<D, 1>());
+      limit((const void*)kv4_weigh_kernel<D, Q_BF16>, weigh_lds<D, Q_BF16>());
+      limit((const void*)kv4_weigh_kernel<D, Q_BF16X2>, weigh_lds<D, Q_BF16X2>());
+      limit((const void*)kv4_weigh_kernel<D, Q_F32>, weigh_lds<D, Q_F32>());
       if (D <= 128) limit((const void*)kv4_attention_kernel<(D <= 128 ? D : 128), Q_BF16, 2>, attn_lds<(D <= 128 ? D : 128), 2>());
     });
   return e == hipSuccess ? 0 : -1;

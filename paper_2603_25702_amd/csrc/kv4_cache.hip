@@ -2,6 +2,8 @@
 // Format and semantics: include/s2d2_kv4.h.  All of it is bound by the bytes it moves.
 #include "kv4.h"
 
+#include <algorithm>
+
 namespace s2d2 {
 
 Kv4 kv4_of(const s2d2_kv4_view* view) {
@@ -143,17 +145,18 @@ void launch_kv4_read(hipStream_t st, int dtype, const Kv4& kv, int N, int T, con
 }
 
 // ---------------------------------------------------------------------------------------------
-// Eviction.  A workgroup per list (sequence, layer, KV head).  The list's masses become integers that order as they do (keys); three
-// histograms of 11, 11 and 10 bits find the key of the budget-th largest; of the entries that hold exactly that key the first ones
-// stay.  Entries below the budget that go are filled from those behind it that stay, in order: places that are written lie below the
-// budget, places that are read behind it, so the moves need no order among themselves, and a list that is a little too long moves a few
-// entries only.
-// A wavefront owns a run of consecutive entries in the walks that need ranks: its counts go through LDS once, ranks inside it
-// come from ballots.
+// Eviction, in two launches.
+//
+// kv4_pick_kernel: a workgroup per list (sequence, layer, KV head).  The list's masses become integers that order as they do (keys), kept in LDS;
+// three histograms of 11, 11 and 10 bits find the key of the budget-th largest; of the entries that hold exactly that key the first ones
+// stay.  Entries below the budget that go are filled from those behind it that stay, in order: the list's moves go to the scratch.
+// A wavefront owns a run of consecutive entries where ranks are needed: its counts go through LDS once, ranks inside it come from ballots.
+// kv4_move_kernel: the moves of all lists by as many workgroups as there are compute units for.  Places that are written lie below the budget,
+// places that are read behind it, so the moves need no order among themselves; and a list that is a little too long moves a few entries only.
 // ---------------------------------------------------------------------------------------------
-static constexpr int EVICT_KEYS = 32768;   // keys kept in LDS; those of longer lists are formed again from memory
-static constexpr int EVICT_MOVES = 2048;   // moves listed at a time
-static constexpr int EVICT_WAVES = 16;
+static constexpr int EVICT_KEYS = 36864;   // keys kept in LDS (144 KB); those of longer lists are formed again from memory
+static constexpr int PICK_SHORT = 8192;    // lists up to here by eight wavefronts
+static constexpr int EVICT_AHEAD = 4;      // entries or moves that a thread has in flight
 
 __device__ __forceinline__ uint32_t evict_key(float mass, int position, int sink, int tail) {
   if (position < sink || position >= tail) return 0xffffffffu;
@@ -163,7 +166,8 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int position, int sink
 }
 
 // Sum over the workgroup's wavefronts before this one, and over all: `mine` of each wavefront (uniform in it).
-__device__ __forceinline__ int waves_before(int mine, int32_t* s /* [EVICT_WAVES] */, int& all) {
+template <int W>
+__device__ __forceinline__ int waves_before(int mine, int32_t* s /* [W] */, int& all) {
   const int wave = threadIdx.x >> 6;
   __syncthreads();
   if ((threadIdx.x & 63) == 0) s[wave] = mine;
@@ -171,7 +175,7 @@ __device__ __forceinline__ int waves_before(int mine, int32_t* s /* [EVICT_WAVES
   int before = 0;
   all = 0;
 #pragma unroll
-  for (int w = 0; w < EVICT_WAVES; ++w) {
+  for (int w = 0; w < W; ++w) {
     const int x = s[w];
     before += w < wave ? x : 0;
     all += x;
@@ -179,30 +183,36 @@ __device__ __forceinline__ int waves_before(int mine, int32_t* s /* [EVICT_WAVES
   return before;
 }
 
-__global__ __launch_bounds__(64 * EVICT_WAVES) void kv4_evict_kernel(Kv4 kv, int budget, int slack, int sink, int recent, int keys) {
+// The moves of a list: count[list] of them (-1: the list is not cut), to[list][m] <- from[list][m], entries of the list.
+struct EvictMoves {
+  int32_t *count, *to, *from;
+  size_t most;   // of a list
+};
+
+template <int W>
+__global__ __launch_bounds__(64 * W, W == 16 ? 8 : 4) void kv4_pick_kernel(Kv4 kv, int budget, int slack, int sink, int recent, int keys, EvictMoves mv) {
   extern __shared__ uint32_t s_mem[];
-  uint32_t* s_key = s_mem;                         // [keys]
-  uint32_t* s_hist = s_key + keys;                 // [2048]
-  uint32_t* s_to = s_hist + 2048;                  // [EVICT_MOVES]
-  uint32_t* s_from = s_to + EVICT_MOVES;           // [EVICT_MOVES]
-  int32_t* s_sum = (int32_t*)(s_from + EVICT_MOVES);   // [EVICT_WAVES]
-  uint32_t* s_pick = (uint32_t*)(s_sum + EVICT_WAVES); // [2]
+  uint32_t* s_key = s_mem;                             // [keys]
+  uint32_t* s_hist = s_key + keys;                     // [2048]
+  int32_t* s_sum = (int32_t*)(s_hist + 2048);          // [W]
+  uint32_t* s_pick = (uint32_t*)(s_sum + W); // [3]: bin, entries of it that stay, entries of it
   const int head = blockIdx.x % kv.H, n = blockIdx.x / kv.H, l = blockIdx.y;
-  const int E = kv.held(n);
-  if (E <= budget || E - budget <= slack) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const size_t list = ((size_t)n * kv.n_layers + l) * kv.H + head;
+  const int E = kv.held(n), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (E <= budget || E - budget <= slack) {
+    if (tid == 0) mv.count[list] = -1;
+    return;
+  }
   const int32_t* pt = kv.page_table + (size_t)n * kv.max_pages;
   const int tail = kv.seq_len[n] - recent;
-  // (a page outside the cache is read as the nearest one)
-  auto entry = [&](int i) __attribute__((always_inline)) {
-    const int p = kv.ps.div(i), page = max(0, min(pt[p], kv.n_pages - 1));
-    return l * kv.layer_entries + kv.at(page, head, i - p * kv.ps.d);
-  };
   auto form = [&](int i) __attribute__((always_inline)) {
-    const size_t at = entry(i);
+    const int p = kv.ps.div(i), page = max(0, min(pt[p], kv.n_pages - 1));   // (a page outside the cache is read as the nearest one)
+    const size_t at = l * kv.layer_entries + kv.at(page, head, i - p * kv.ps.d);
     return evict_key(kv.mass[at], kv.position[at], sink, tail);
   };
   auto key = [&](int i) __attribute__((always_inline)) { return i < keys ? s_key[i] : form(i); };
+  auto key_of = [&](int i) __attribute__((always_inline)) { return i < E ? key(i) : 0u; };
+  constexpr int STEP = 64 * W;
 
   // ---- the budget-th largest key ----
   uint32_t prefix = 0;
@@ -210,41 +220,51 @@ __global__ __launch_bounds__(64 * EVICT_WAVES) void kv4_evict_kernel(Kv4 kv, int
   int shift = 32;
   for (int pass = 0; pass < 3; ++pass) {
     const int bits = pass < 2 ? 11 : 10;
-    for (int i = tid; i < 2048; i += 64 * EVICT_WAVES) s_hist[i] = 0;
+    for (int i = tid; i < 2048; i += STEP) s_hist[i] = 0;
     __syncthreads();
-    for (int i0 = 0; i0 < E; i0 += 64 * EVICT_WAVES) {
-      const int i = i0 + tid;
-      bool counts = i < E;
-      uint32_t k = 0;
-      if (counts) {
-        k = pass == 0 ? form(i) : key(i);
-        if (pass == 0 && i < keys) s_key[i] = k;
-        counts = pass == 0 || (k >> shift) == prefix;
-      }
-      const int bin = (int)((k >> (shift - bits)) & ((1u << bits) - 1));
-      // entries without weight share a bin: the lanes that agree with the first one add once
-      const unsigned long long who = __ballot(counts);
-      if (who) {
-        const int lead = __ffsll((long long)who) - 1, first = __builtin_amdgcn_readlane(bin, lead);
-        const unsigned long long same = __ballot(counts && bin == first);
-        if (lane == lead) atomicAdd(&s_hist[first], (uint32_t)__popcll(same));
-        else if (counts && bin != first) atomicAdd(&s_hist[bin], 1u);
+    for (int i0 = tid; i0 - tid < E; i0 += EVICT_AHEAD * STEP) {
+      uint32_t k[EVICT_AHEAD];
+      if (pass == 0) {
+#pragma unroll
+        for (int u = 0; u < EVICT_AHEAD; ++u) k[u] = form(min(i0 + u * STEP, E - 1));
+#pragma unroll
+        for (int u = 0; u < EVICT_AHEAD; ++u)
+          if (i0 + u * STEP < min(E, keys)) s_key[i0 + u * STEP] = k[u];
+      } else
+#pragma unroll
+        for (int u = 0; u < EVICT_AHEAD; ++u) k[u] = key_of(i0 + u * STEP);
+#pragma unroll
+      for (int u = 0; u < EVICT_AHEAD; ++u) {
+        const bool counts = i0 + u * STEP < E && (pass == 0 || (k[u] >> shift) == prefix);
+        const int bin = (int)((k[u] >> (shift - bits)) & ((1u << bits) - 1));
+        // entries without weight share a bin: the lanes that agree with the first one add once
+        const unsigned long long who = __ballot(counts);
+        if (who) {
+          const int lead = __ffsll((long long)who) - 1, first = __builtin_amdgcn_readlane(bin, lead);
+          const unsigned long long same = __ballot(counts && bin == first);
+          if (lane == lead) atomicAdd(&s_hist[first], (uint32_t)__popcll(same));
+          else if (counts && bin != first) atomicAdd(&s_hist[bin], 1u);
+        }
       }
     }
     __syncthreads();
-    // counts from the top: thread t holds bins 2047 - 2 t and 2046 - 2 t
-    const int b = 2047 - 2 * tid;
-    const int x0 = (int)s_hist[b], x1 = (int)s_hist[b - 1];
-    int incl = x0 + x1;
+    // counts from the top: thread t holds bins 2047 - BINS t and on downwards
+    constexpr int BINS = 2048 / STEP;
+    int x[BINS], mine = 0;
+#pragma unroll
+    for (int u = 0; u < BINS; ++u) { x[u] = (int)s_hist[2047 - BINS * tid - u]; mine += x[u]; }
+    int incl = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const int y = __shfl_up(incl, off, 64);
       if (lane >= off) incl += y;
     }
-    int all;
-    const int above = waves_before(__builtin_amdgcn_readlane(incl, 63), s_sum, all) + incl - x0 - x1;
-    if (above < need && above + x0 >= need) { s_pick[0] = b; s_pick[1] = need - above; }
-    else if (above + x0 < need && above + x0 + x1 >= need) { s_pick[0] = b - 1; s_pick[1] = need - above - x0; }
+    int all, above = waves_before<W>(__builtin_amdgcn_readlane(incl, 63), s_sum, all) + incl - mine;
+#pragma unroll
+    for (int u = 0; u < BINS; ++u) {
+      if (above < need && above + x[u] >= need) { s_pick[0] = 2047 - BINS * tid - u; s_pick[1] = need - above; s_pick[2] = x[u]; }
+      above += x[u];
+    }
     __syncthreads();
     shift -= bits;
     prefix = (prefix << bits) | s_pick[0];
@@ -253,83 +273,120 @@ __global__ __launch_bounds__(64 * EVICT_WAVES) void kv4_evict_kernel(Kv4 kv, int
   const uint32_t last = prefix;   // of the entries with this key the first `need` stay
 
   // ---- who stays: wavefront w walks entries [w0, w1) ----
-  const int run = ((E + 64 * EVICT_WAVES - 1) / (64 * EVICT_WAVES)) * 64, w0 = min(E, wave * run), w1 = min(E, w0 + run);
+  const int run = ((E + STEP - 1) / STEP) * 64, w0 = min(E, wave * run), w1 = min(E, w0 + run);
   auto lanes_below = [&](unsigned long long m) __attribute__((always_inline)) { return __popcll(m & ((1ull << lane) - 1)); };
-  int equal = 0, all;
-  for (int i = w0 + lane; i - lane < w1; i += 64) equal += __popcll(__ballot(i < w1 && key(i) == last));
-  const int equal0 = waves_before(equal, s_sum, all);
-  // calls put(entry, whether it stays) for the wavefront's entries in order, all lanes together
+  int all, equal0 = 0;
+  const bool tied = (int)s_pick[2] != need;   // some entries with the last key go
+  if (tied) {
+    int equal = 0;
+    for (int i = w0 + lane; i - lane < w1; i += 64) equal += __popcll(__ballot(i < w1 && key(i) == last));
+    equal0 = waves_before<W>(equal, s_sum, all);
+  }
+  // calls put(entry, whether it goes and is written, whether it stays and is read) for the wavefront's entries in order, all lanes together
   auto walk = [&](auto put) __attribute__((always_inline)) {
     int seen = equal0;
-    for (int i = w0 + lane; i - lane < w1; i += 64) {
-      const bool in = i < w1;
-      const uint32_t k = in ? key(i) : 0u;
-      const unsigned long long eq = __ballot(in && k == last);
-      const bool stays = in && (k > last || (k == last && seen + lanes_below(eq) < need));
-      seen += __popcll(eq);
-      put(i, in, stays);
+    for (int i0 = w0 + lane; i0 - lane < w1; i0 += 64 * EVICT_AHEAD) {
+      uint32_t k[EVICT_AHEAD];
+#pragma unroll
+      for (int u = 0; u < EVICT_AHEAD; ++u) k[u] = key_of(i0 + 64 * u);
+#pragma unroll
+      for (int u = 0; u < EVICT_AHEAD; ++u) {
+        const int i = i0 + 64 * u;
+        const bool in = i < w1;
+        bool stays = in && k[u] >= last;
+        if (tied) {
+          const unsigned long long eq = __ballot(in && k[u] == last);
+          if (k[u] == last && seen + lanes_below(eq) >= need) stays = false;
+          seen += __popcll(eq);
+        }
+        put(i, in && i < budget && !stays, stays && i >= budget);
+      }
     }
   };
   int holes = 0, kept = 0;
-  walk([&](int i, bool in, bool stays) __attribute__((always_inline)) {
-    holes += __popcll(__ballot(in && i < budget && !stays));
-    kept += __popcll(__ballot(stays && i >= budget));
+  walk([&](int, bool hole, bool source) __attribute__((always_inline)) {
+    holes += __popcll(__ballot(hole));
+    kept += __popcll(__ballot(source));
   });
   int moves;
-  const int holes0 = waves_before(holes, s_sum, moves), kept0 = waves_before(kept, s_sum, all);
-  moves = min(moves, all);   // (the same number)
+  int hole0 = waves_before<W>(holes, s_sum, moves), kept0 = waves_before<W>(kept, s_sum, all);   // (as many of one as of the other)
+  int32_t *to = mv.to + list * mv.most, *from = mv.from + list * mv.most;
+  walk([&](int i, bool hole, bool source) __attribute__((always_inline)) {
+    const unsigned long long goes = __ballot(hole), comes = __ballot(source);
+    if (hole) to[hole0 + lanes_below(goes)] = i;
+    if (source) from[kept0 + lanes_below(comes)] = i;
+    hole0 += __popcll(goes);
+    kept0 += __popcll(comes);
+  });
+  if (tid == 0) mv.count[list] = moves;
+}
 
-  // ---- the moves, so many at a time ----
-  const int codes = kv.D / 32, items = 2 * codes + 4, width = items <= 8 ? 8 : items <= 16 ? 16 : 32;   // 16-byte pieces of K and V; scales, mass, position
-  for (int m0 = 0; m0 < moves; m0 += EVICT_MOVES) {
-    __syncthreads();
-    int hole = holes0 - m0, keep = kept0 - m0;
-    walk([&](int i, bool in, bool stays) __attribute__((always_inline)) {
-      const unsigned long long goes = __ballot(in && i < budget && !stays), comes = __ballot(stays && i >= budget);
-      const int a = hole + lanes_below(goes), b = keep + lanes_below(comes);
-      if (in && i < budget && !stays && a >= 0 && a < EVICT_MOVES) s_to[a] = i;
-      if (stays && i >= budget && b >= 0 && b < EVICT_MOVES) s_from[b] = i;
-      hole += __popcll(goes);
-      keep += __popcll(comes);
-    });
-    __syncthreads();
-    const int now = min(EVICT_MOVES, moves - m0), j = tid % width;
-    for (int m = tid / width; m < now; m += 64 * EVICT_WAVES / width) {
-      const int to = (int)s_to[m];
-      const int page = pt[kv.ps.div(to)];
-      if (page < 0 || page >= kv.n_pages) continue;
-      const size_t a = entry(to), b = entry((int)s_from[m]);
-      if (j < 2 * codes) {
-        uint8_t* base = j < codes ? kv.kc : kv.vc;
-        const int piece = j < codes ? j : j - codes;
-        ((uint4*)(base + a * (kv.D / 2)))[piece] = ((const uint4*)(base + b * (kv.D / 2)))[piece];
-      } else if (j < 2 * codes + 2) {
-        uint8_t* base = j == 2 * codes ? kv.ks : kv.vs;
-        for (int g = 0; g < codes; ++g) base[a * codes + g] = base[b * codes + g];
-      } else if (j == 2 * codes + 2) kv.mass[a] = kv.mass[b];
-      else if (j == 2 * codes + 3) kv.position[a] = kv.position[b];
+// width: threads of a move, enough for the 16-byte pieces of K and V and for scales, mass and position (a power of two); per_list: workgroups
+__global__ __launch_bounds__(256) void kv4_move_kernel(Kv4 kv, int budget, int width, int per_list, EvictMoves mv) {
+  const size_t list = blockIdx.x / per_list;
+  const int slice = blockIdx.x % per_list, head = (int)(list % kv.H), l = (int)(list / kv.H % kv.n_layers), n = (int)(list / kv.H / kv.n_layers);
+  const int moves = mv.count[list];
+  if (moves < 0) return;
+  if (l == 0 && head == 0 && slice == 0 && threadIdx.x == 0) kv.entries[n] = budget;
+  const int codes = kv.D / 32, j = threadIdx.x % width, step = 256 / width * per_list;
+  if (j >= 2 * codes + 4) return;
+  const int32_t *pt = kv.page_table + (size_t)n * kv.max_pages, *to_of = mv.to + list * mv.most, *from_of = mv.from + list * mv.most;
+  for (int m0 = slice * (256 / width) + threadIdx.x / width; m0 < moves; m0 += EVICT_AHEAD * step) {
+    size_t to[EVICT_AHEAD], from[EVICT_AHEAD];
+    bool there[EVICT_AHEAD];
+#pragma unroll
+    for (int u = 0; u < EVICT_AHEAD; ++u) {
+      const int m = min(m0 + u * step, moves - 1), a = to_of[m], b = from_of[m], pa = kv.ps.div(a), pb = kv.ps.div(b), page = pt[pa];
+      there[u] = m0 + u * step < moves && page >= 0 && page < kv.n_pages;   // (a page outside the cache is never written)
+      to[u] = l * kv.layer_entries + kv.at(max(0, min(page, kv.n_pages - 1)), head, a - pa * kv.ps.d);
+      from[u] = l * kv.layer_entries + kv.at(max(0, min(pt[pb], kv.n_pages - 1)), head, b - pb * kv.ps.d);
+    }
+    auto move = [&](auto word, void* base, int per_entry, int piece) __attribute__((always_inline)) {
+      using W = decltype(word);
+      W x[EVICT_AHEAD];
+#pragma unroll
+      for (int u = 0; u < EVICT_AHEAD; ++u) x[u] = ((const W*)base)[from[u] * per_entry + piece];
+#pragma unroll
+      for (int u = 0; u < EVICT_AHEAD; ++u)
+        if (there[u]) ((W*)base)[to[u] * per_entry + piece] = x[u];
+    };
+    if (j < 2 * codes) move(u32x4_t{}, j < codes ? kv.kc : kv.vc, codes, j < codes ? j : j - codes);
+    else if (j >= 2 * codes + 2) move(uint32_t{}, j == 2 * codes + 2 ? (void*)kv.mass : (void*)kv.position, 1, 0);
+    else {   // the scales of an entry: one word of 1, 2, 4 or 8 bytes
+      void* base = j == 2 * codes ? kv.ks : kv.vs;
+      if (codes == 1) move(uint8_t{}, base, 1, 0);
+      else if (codes == 2) move(uint16_t{}, base, 1, 0);
+      else if (codes == 4) move(uint32_t{}, base, 1, 0);
+      else move(uint64_t{}, base, 1, 0);
     }
   }
 }
 
-__global__ void kv4_evict_commit_kernel(Kv4 kv, int N, int budget, int slack) {
-  const int n = blockIdx.x * blockDim.x + threadIdx.x;
-  if (n >= N) return;
-  const int E = kv.held(n);
-  if (E > budget && E - budget > slack) kv.entries[n] = budget;
+static size_t pick_lds(int keys) { return ((size_t)keys + 2048 + 16 + 3) * sizeof(uint32_t); }
+
+// A list has at most as many moves as entries below the budget, and as behind it: half its places.
+size_t kv4_evict_bytes(const Kv4& kv, int N) {
+  const size_t lists = (size_t)N * kv.n_layers * kv.H;
+  return (lists * (1 + 2 * (size_t)(kv.cap / 2)) * sizeof(int32_t) + 255) & ~(size_t)255;
 }
 
-static size_t evict_lds(int keys) { return ((size_t)keys + 2048 + 2 * EVICT_MOVES + EVICT_WAVES + 2) * sizeof(uint32_t); }
-
-void launch_kv4_evict(hipStream_t st, const Kv4& kv, int N, int budget, int slack, int sink, int recent) {
-  const int keys = kv.cap < EVICT_KEYS ? kv.cap : EVICT_KEYS;
-  S2D2_LAUNCH(kv4_evict_kernel, dim3(N * kv.H, kv.n_layers), dim3(64 * EVICT_WAVES), evict_lds(keys), st, kv, budget, slack, sink, recent, keys);
-  S2D2_LAUNCH(kv4_evict_commit_kernel, dim3((N + 255) / 256), dim3(256), 0, st, kv, N, budget, slack);
+void launch_kv4_evict(hipStream_t st, const Kv4& kv, int N, int budget, int slack, int sink, int recent, void* scratch) {
+  const int keys = kv.cap < EVICT_KEYS ? kv.cap : EVICT_KEYS, most = std::min(budget, kv.cap - budget);
+  if (most <= 0) return;   // (no list is longer)
+  const size_t lists = (size_t)N * kv.n_layers * kv.H;
+  EvictMoves mv{(int32_t*)scratch, (int32_t*)scratch + lists, nullptr, (size_t)most};
+  mv.from = mv.to + lists * mv.most;
+  const dim3 grid(N * kv.H, kv.n_layers);
+  if (kv.cap <= PICK_SHORT) S2D2_LAUNCH(kv4_pick_kernel<8>, grid, dim3(512), pick_lds(keys), st, kv, budget, slack, sink, recent, keys, mv);
+  else S2D2_LAUNCH(kv4_pick_kernel<16>, grid, dim3(1024), pick_lds(keys), st, kv, budget, slack, sink, recent, keys, mv);
+  const int codes = kv.D / 32, width = 2 * codes + 4 <= 8 ? 8 : 2 * codes + 4 <= 16 ? 16 : 32, at_once = 256 / width * EVICT_AHEAD;
+  const int per_list = std::max(1, std::min((int)((2048 + lists - 1) / lists), (most + at_once - 1) / at_once));
+  S2D2_LAUNCH(kv4_move_kernel, dim3((unsigned)(lists * per_list)), dim3(256), 0, st, kv, budget, width, per_list, mv);
 }
 
 // LDS above 64 KB has to be asked for, once a device.
 int kv4_evict_init() {
-  return hipFuncSetAttribute((const void*)kv4_evict_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)evict_lds(EVICT_KEYS)) != hipSuccess;
+  return hipFuncSetAttribute((const void*)kv4_pick_kernel<16>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)pick_lds(EVICT_KEYS)) != hipSuccess;
 }
 
 }  // namespace s2d2

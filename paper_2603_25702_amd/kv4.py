@@ -13,7 +13,7 @@ import torch
 
 from .binding import S2D2_BF16, S2D2_EINVAL, S2D2_F32, KvView, S2D2Error, _check, _ptr, load_library
 
-EXPORTS = ["s2d2_kv4_append", "s2d2_kv4_read", "s2d2_kv4_attention_bytes", "s2d2_kv4_attention", "s2d2_kv4_weigh", "s2d2_kv4_evict", "s2d2_set_kv4"]
+EXPORTS = ["s2d2_kv4_append", "s2d2_kv4_read", "s2d2_kv4_attention_bytes", "s2d2_kv4_attention", "s2d2_kv4_weigh", "s2d2_kv4_evict_bytes", "s2d2_kv4_evict", "s2d2_set_kv4"]
 GROUP = 32   # values that share a power of two
 
 
@@ -44,7 +44,8 @@ def _lib():
         lib.s2d2_kv4_attention_bytes.argtypes = [view, i32, i32, i32]
         lib.s2d2_kv4_attention.argtypes = [p, view, i32, rows, p, C.c_size_t]
         lib.s2d2_kv4_weigh.argtypes = [p, view, i32, rows]
-        lib.s2d2_kv4_evict.argtypes = [p, view, i32, i32, i32, i32, i32]
+        lib.s2d2_kv4_evict_bytes.argtypes = [view, i32]
+        lib.s2d2_kv4_evict.argtypes = [p, view, i32, i32, i32, i32, i32, p, C.c_size_t]
         lib.s2d2_set_kv4.argtypes = [p, view, p, C.c_size_t, p]
         for n in EXPORTS:
             getattr(lib, n).restype = C.c_int64 if n.endswith("_bytes") else C.c_int32
@@ -75,7 +76,7 @@ def _rows_layout(t: torch.Tensor, name: str, rows: int, heads: int, dim: int, dt
 
 class Kv4Cache:
     """k_codes, v_codes uint8 [n_layers, n_pages, Hkv, page_size, D / 2]; k_scales, v_scales uint8 [.., D / 32]; mass fp32 and position int32
-    [n_layers, n_pages, Hkv, page_size] or None; page_table int32 [N, max_pages]; entries, seq_len, status int32 [N]."""
+    [n_layers, n_pages, Hkv, page_size] or None (both: an eviction scratch of 4 bytes a place and list comes with them); page_table int32 [N, max_pages]; entries, seq_len, status int32 [N]."""
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales, page_table, entries, seq_len, status=None, mass=None, position=None):
         if k_codes.dim() != 5 or k_codes.dtype != torch.uint8:
@@ -102,6 +103,12 @@ class Kv4Cache:
         self._view = Kv4View(*[_ptr(t) for t in (k_codes, v_codes, k_scales, v_scales, mass, position, page_table, entries, seq_len, status)],
                              self.n_layers, self.n_pages, self.page_size, page_table.shape[1], self.n_kv_heads, self.head_dim)
         self._ref = C.byref(self._view)
+        self.moves = None   # scratch of the eviction, with mass and position
+        if mass is not None and position is not None:
+            n = _lib().s2d2_kv4_evict_bytes(self._ref, self.N)
+            if n < 0:
+                raise S2D2Error(int(n), _LIB.s2d2_last_error().decode())
+            self.moves = torch.empty(int(n), dtype=torch.uint8, device=self.device)
 
     @staticmethod
     def alloc(n_layers: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, page_table: torch.Tensor, weights: bool = False) -> "Kv4Cache":
@@ -218,9 +225,10 @@ def s2d2_kv4_weigh(kv: Kv4Cache, layer: int, rows: Kv4Rows, stream: Optional[tor
 
 
 def s2d2_kv4_evict(kv: Kv4Cache, budget: int, slack: int = 0, sink: int = 0, recent: int = 0, stream: Optional[torch.cuda.Stream] = None):
-    """Cuts the sequences with more than budget + slack entries to `budget` of them, list by list."""
+    """Cuts the sequences with more than budget + slack entries to `budget` of them, list by list; the scratch is the cache's own."""
     lib = _LIB or _lib()
-    kv._call(lib.s2d2_kv4_evict, stream, kv.N, budget, slack, sink, recent)
+    moves = kv.moves
+    kv._call(lib.s2d2_kv4_evict, stream, kv.N, budget, slack, sink, recent, _ptr(moves), 0 if moves is None else moves.numel())
 
 
 def s2d2_set_kv4(eng, kv: Optional[Kv4Cache]):

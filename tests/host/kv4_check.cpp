@@ -36,7 +36,7 @@ int main() {
       EXPECT(b >= 0 || b == S2D2_EINVAL);
       // (a scratch that is always too small, a layer that is never there, a budget that is never allowed: nothing is launched)
       EXPECT(s2d2_kv4_attention(nullptr, &w, -1, &rows, fake, 0) == S2D2_EINVAL);
-      EXPECT(s2d2_kv4_evict(nullptr, &w, 16, 0, 0, 0, 0) == S2D2_EINVAL);
+      EXPECT(s2d2_kv4_evict(nullptr, &w, 16, 0, 0, 0, 0, fake, SIZE_MAX) == S2D2_EINVAL && s2d2_kv4_evict_bytes(&w, 1024) != 0);
       EXPECT(s2d2_kv4_append(nullptr, &w, 16, 32, 512, 9, fake, fake, 0, 0, ints, ints) == S2D2_EINVAL);
       EXPECT(s2d2_kv4_read(nullptr, &w, 16, 32, 9, ints, fake, fake) == S2D2_EINVAL);
     }
@@ -66,7 +66,8 @@ int main() {
   }
   for (int32_t a : extremes)
     for (int32_t b : extremes)
-      if (a < 0 || b < 0 || (int64_t)a + b > 8) EXPECT(s2d2_kv4_evict(nullptr, &good, 16, 8, 0, a, b) == S2D2_EINVAL);
+      if (a < 0 || b < 0 || (int64_t)a + b > 8) EXPECT(s2d2_kv4_evict(nullptr, &good, 16, 8, 0, a, b, fake, SIZE_MAX) == S2D2_EINVAL);
+      else EXPECT(s2d2_kv4_evict(nullptr, &good, 16, 8, 0, a, b, fake, 8) == S2D2_ENOSPC);
   EXPECT(s2d2_kv4_attention_bytes(nullptr, 1, 1, 8) == S2D2_EINVAL);
   EXPECT(s2d2_set_kv4(nullptr, &good, fake, 0, nullptr) == S2D2_EINVAL && s2d2_set_kv4(nullptr, nullptr, nullptr, 0, nullptr) == S2D2_EINVAL);
 

@@ -64,7 +64,8 @@ def test_bad_caches_are_refused_by_every_call(lib, field, value):
     assert lib.s2d2_kv4_attention_bytes(w, 4, 8, 32) == EINVAL
     assert lib.s2d2_kv4_attention(None, w, 0, rows(), FAKE, 1 << 40) == EINVAL
     assert lib.s2d2_kv4_weigh(None, w, 0, rows()) == EINVAL
-    assert lib.s2d2_kv4_evict(None, w, 4, 100, 0, 0, 0) == EINVAL
+    assert lib.s2d2_kv4_evict(None, w, 4, 100, 0, 0, 0, FAKE, 1 << 40) == EINVAL
+    assert lib.s2d2_kv4_evict_bytes(w, 4) == EINVAL
     assert b"4-bit cache" in lib.s2d2_last_error()
 
 
@@ -101,9 +102,14 @@ def test_other_refusals(lib):
     assert lib.s2d2_kv4_weigh(None, view(mass=None), 0, rows()) == EINVAL
     for n, budget, slack, sink, recent in ((0, 8, 0, 0, 0), (1025, 8, 0, 0, 0), (4, 0, 0, 0, 0), (4, 8, -1, 0, 0), (4, 8, 0, -1, 0), (4, 8, 0, 0, -1), (4, 8, 0, 5, 4),
                                            (4, 8, 0, 2**31 - 1, 2**31 - 1)):
-        assert lib.s2d2_kv4_evict(None, w, n, budget, slack, sink, recent) == EINVAL
-    assert lib.s2d2_kv4_evict(None, view(mass=None), 4, 8, 0, 0, 0) == EINVAL
-    assert lib.s2d2_kv4_evict(None, view(position=None), 4, 8, 0, 0, 0) == EINVAL
+        assert lib.s2d2_kv4_evict(None, w, n, budget, slack, sink, recent, FAKE, 1 << 40) == EINVAL
+    assert lib.s2d2_kv4_evict(None, view(mass=None), 4, 8, 0, 0, 0, FAKE, 1 << 40) == EINVAL
+    assert lib.s2d2_kv4_evict(None, view(position=None), 4, 8, 0, 0, 0, FAKE, 1 << 40) == EINVAL
+    need = lib.s2d2_kv4_evict_bytes(w, 4)
+    assert need >= 4 * 2 * 4 * 8 * (1 + 32 * 16) and lib.s2d2_kv4_evict_bytes(w, 0) == EINVAL
+    assert lib.s2d2_kv4_evict(None, w, 4, 8, 0, 0, 0, FAKE, need - 1) == ENOSPC
+    assert lib.s2d2_kv4_evict(None, w, 4, 8, 0, 0, 0, FAKE + 2, need) == EINVAL
+    assert lib.s2d2_kv4_evict(None, w, 4, 8, 0, 0, 0, None, need) == EINVAL
     good = (w, 4, 8, 32, 1, FAKE, FAKE, 1 << 20, 1024, FAKE, FAKE)
     for at, bad in ((1, 0), (1, 1025), (2, 0), (3, 0), (4, 7), (5, None), (5, FAKE + 8), (6, None), (7, 512), (7, 1025 * 1024 + 4), (7, -1024), (8, 1016), (8, 1028), (9, None), (10, FAKE + 2)):
         assert lib.s2d2_kv4_append(None, *good[:at], bad, *good[at + 1:]) == EINVAL, at
