@@ -31,8 +31,9 @@ static constexpr float LN2 = 0.69314718055994530942f;
 static constexpr float LOWEST = -3.402823466e38f;   // reference of a row that has seen nothing
 static constexpr float BELOW = 7.f;                 // a reference is taken this far below a maximum (base 2)
 static constexpr float MOST = 32768.f;              // and moves when the weights of a tile of keys sum up to more
-static constexpr int ATT_WAVES = 8;
-static constexpr int MIN_RUN = 32;                  // tiles of a split, at least: four a wavefront
+// Wavefronts of a workgroup.  Heads of 256 take 128 registers for the output alone: four wavefronts of up to 512 registers, else eight of up to 256.
+constexpr int waves_of(int D) { return D == 256 ? 4 : 8; }
+constexpr int min_run_of(int D) { return 4 * waves_of(D); }   // tiles of a split, at least: four a wavefront
 
 enum QueryMode { Q_BF16 = 0, Q_BF16X2 = 1, Q_F32 = 2 };
 template <int QM> struct Mode;
@@ -118,11 +119,18 @@ __device__ __forceinline__ SeqTiles seq_tiles(const Kv4Attn& a, int n) {
   s.tiles = s.cached + (a.k ? (rows + 31) >> 5 : 0);
   return s;
 }
-__device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+// Inclusive sums over the lanes by DPP moves (vector-ALU operands, no trips through LDS): inside the rows of 16 lanes, then lane 15 of
+// rows 0 and 2 to the next row, then lane 31 to the upper half.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31
   return v;
 }
+__device__ __forceinline__ int wave_sum(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
 __device__ __forceinline__ int splits_of_seq(const SeqTiles& s, int run) { return s.rows == 0 ? 0 : max(1, (s.tiles + run - 1) / run); }
 
 // Tiles of a split.  The batch's tiles over the workgroups that are resident at once (target), less half a split a sequence, since the last split of each
@@ -139,16 +147,11 @@ __device__ __forceinline__ bool find_item(const Kv4Attn& a, int w, int lane, Ite
   SeqTiles s = seq_tiles(a, lane);
   int total = s.tiles;
   for (int n0 = 64; n0 < a.N; n0 += 64) total += seq_tiles(a, n0 + lane).tiles;
-  it.run = run_of(a, __builtin_amdgcn_readfirstlane(wave_sum(total)));
+  it.run = run_of(a, wave_sum(total));
   int before = 0;
   for (int n0 = 0;;) {
     const int mine = splits_of_seq(s, it.run);
-    int incl = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int y = __shfl_up(incl, off, 64);
-      if (lane >= off) incl += y;
-    }
+    const int incl = wave_scan(mine);
     const unsigned long long hit = __ballot(w - before < incl && w - before >= incl - mine);
     if (hit) {
       const int src = __ffsll((long long)hit) - 1;
@@ -241,16 +244,18 @@ struct RowState {
   }
 };
 
+// V in LDS: a row of D half values a key, rows 2 D + 64 bytes apart, bit 5 of a byte's place in its row flipped in keys with bit 3 set.  Then neither the
+// 16-byte writes (8 lanes: keys k .. k + 3 and k + 8 .. k + 11) nor the transposing reads (32 lanes: 64 bytes of keys k .. k + 3) meet in a bank.
 template <int D>
-static constexpr int V_LD = 2 * D + 32;   // bytes of a key's row of V in LDS: 16 lanes of a transposing read touch four rows, which then lie in different banks
+static constexpr int V_LD = 2 * D + 64;
 
 // QT == 1: queries in registers, the next tile's codes requested a tile ahead.  QT == 2: the conversion of K and V serves two query tiles;
 // their outputs take 128 registers, so the queries stay in LDS (one copy for the workgroup, in operand order) and the next codes are requested
 // into the registers of the converted ones.
 template <int D, int QM, int QT>
-__global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4Attn a, int layer) {
+__global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const Kv4Attn a, int layer) {
   typedef typename Mode<QM>::T T;
-  constexpr int QP = Mode<QM>::QP, PP = Mode<QM>::PP, WP = Mode<QM>::WP, WPP = Mode<QM>::WPP, NW = ATT_WAVES, DT = D / 32, DS = D / 16;
+  constexpr int QP = Mode<QM>::QP, PP = Mode<QM>::PP, WP = Mode<QM>::WP, WPP = Mode<QM>::WPP, NW = waves_of(D), DT = D / 32, DS = D / 16;
   constexpr bool Q_LDS = QT > 1;
   extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
@@ -266,7 +271,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
   const int t0 = it.z * it.run, t1 = min(sq.tiles, t0 + it.run), c1 = min(t1, sq.cached);
   const int tiles_q = min(QT, (nq - q0 + 31) / 32);
 
-  // ---- cached keys: lane (c, h) takes half h of key tile_key(c) of a tile ----
+  // Cached keys: lane (c, h) takes half h of key tile_key(c) of a tile.
   const int kperm = tile_key(c);
   const int32_t* pt = kv.page_table + (size_t)it.n * kv.max_pages;
   const uint8_t *kc = kv.kc + layer * kv.layer_entries * (D / 2), *vc = kv.vc + layer * kv.layer_entries * (D / 2);
@@ -315,14 +320,17 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
   uint8_t* s_v = s_mem + (size_t)wave * 32 * V_LD<D>;   // this wavefront's tile of V
   const int g16 = lane >> 4, i16 = lane & 15;
   // transposing read: 16 lanes take 16 dimensions of 4 keys; lanes 0-31 keys 0-7, lanes 32-63 keys 8-15 of a step
-  const uint8_t* s_tr = s_v + (8 * (g16 >> 1) + (i16 >> 2)) * V_LD<D> + ((g16 & 1) * 16 + (i16 & 3) * 4) * 2;
+  const uint8_t* s_tr = s_v + (8 * h + (i16 >> 2)) * V_LD<D> + ((g16 & 1) ^ h) * 32 + (i16 & 3) * 8;
   auto v_operand = [&](int dt, int j) __attribute__((always_inline)) {
     const uint8_t* p = s_tr + 16 * j * V_LD<D> + dt * 64;
     const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)p), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(p + 4 * V_LD<D>));
     const uint2 u = __builtin_bit_cast(uint2, x), v = __builtin_bit_cast(uint2, y);
     return u32x4_t{u.x, u.y, v.x, v.y};
   };
-  u32x4_t* s_vrow = (u32x4_t*)(s_v + kperm * V_LD<D> + h * D);   // this lane's half row of V
+  // this lane's half row of V: the 16 bytes of word i
+  const int flip = (kperm >> 3) & 1;
+  uint8_t* s_vrow = s_v + kperm * V_LD<D> + (D == 32 ? (h ^ flip) * 32 : h * D);
+  auto v_word = [&](int i) __attribute__((always_inline)) -> u32x4_t& { return *(u32x4_t*)(s_vrow + 16 * i + (D == 32 ? 0 : i & 2 ? -32 * flip : 32 * flip)); };
   auto lds_written = []() __attribute__((always_inline)) {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -332,7 +340,8 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
     __builtin_amdgcn_wave_barrier();
   };
 
-  // One tile of cached keys from k, v.  after_v(), after_k() run once V and K are converted.  Queries in LDS: the first half of a tile's operands is
+  // One tile of cached keys from k, v.  after_v(), after_k() run once V and K are converted.  The matrix instructions go ahead of the other
+  // wavefront's vector work (s_setprio; 2 % of the verification windows).  Queries in LDS: the first half of a tile's operands is
   // requested before V is converted, every further one when its predecessor's registers are free.
   auto cached_tile = [&](int tile, const HalfRow<D>& k, HalfRow<D>& v, auto after_v, auto after_k) __attribute__((always_inline)) {
     constexpr int AHEAD = Q_LDS ? (DS < 4 ? DS : 4) : 1;
@@ -349,9 +358,10 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
     const bool part = tile * 32 + 32 > sq.S;
     if (part && tile * 32 + kperm >= sq.S) v.clear();   // (what lies behind the entries may be anything)
 #pragma unroll
-    for (int i = 0; i < DS; ++i) s_vrow[i] = codes_f16(v.w[i], v.scale(i));
+    for (int i = 0; i < DS; ++i) v_word(i) = codes_f16(v.w[i], v.scale(i));
     lds_written();
     after_v();
+    __builtin_amdgcn_s_setprio(1);
     f32x16_t s[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t)
@@ -369,6 +379,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
         }
       if (Q_LDS) __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     after_k();
     u32x4_t pw[QT][2][PP];
 #pragma unroll
@@ -395,6 +406,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
           }
         }
     }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -405,39 +417,21 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
 #pragma unroll
           for (int e = 0; e < PP; ++e) st[t].o[dt] = mfma_f16(vf, pw[t][j][e], st[t].o[dt]);
       }
+    __builtin_amdgcn_s_setprio(0);
     lds_read();
   };
-  if (tile < c1) {
-    request(tile);
-    if (tile + NW < c1) request_page(tile + NW);
-  }
-  if (Q_LDS) __syncthreads();
-  if (Q_LDS) {
-    size_t at = 0;
-    for (; tile < c1; tile += NW)
-      cached_tile(tile, kn, vn, [&]() __attribute__((always_inline)) {
-        if (tile + NW < c1) {
-          at = entry_of(tile + NW);
-          vn.load(vc, vs, at, h);
-          if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
-        }
-      }, [&]() __attribute__((always_inline)) {
-        if (tile + NW < c1) kn.load(kc, ks, at, h);
-      });
-  } else {
-    for (; tile < c1; tile += NW) {
-      const HalfRow<D> k = kn;
-      HalfRow<D> v = vn;
-      if (tile + NW < c1) {
-        request(tile + NW);
-        if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
-      }
-      cached_tile(tile, k, v, []() {}, []() {});
+  auto first = [&]() __attribute__((always_inline)) {
+    if (tile < c1) {
+      request(tile);
+      if (tile + NW < c1) request_page(tile + NW);
     }
-  }
+  };
+  constexpr bool EARLY = QT == 1 && QM != Q_F32;   // codes on their way while the window is computed: 18 registers that the others have not
+  if (EARLY) first();
+  if (Q_LDS) __syncthreads();
 
-  // ---- the window's own keys: V plane by plane through LDS ----
-  for (; tile < t1; tile += NW) {
+  // ---- the window's own keys: V plane by plane through LDS.  The last wavefronts first: they have the fewer cached tiles ----
+  for (int tile = max(t0, sq.cached) + NW - 1 - wave; tile < t1; tile += NW) {
     const int base = (tile - sq.cached) * 32, key = base + kperm;
     const bool there = key < sq.rows;
     const int64_t at = (int64_t)(sq.row0 + min(key, sq.rows - 1)) * a.kv_ld + kvh * D + h * (D / 2);
@@ -448,14 +442,14 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
       load_planes<WP>((const T*)a.v + at + 8 * ds, 0, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i) bad |= (v[0][i] & 0x7f80u) == 0x7f80u || (v[0][i] & 0x7f800000u) == 0x7f800000u;
-      s_vrow[ds] = there ? v[0] : u32x4_t{0, 0, 0, 0};
+      v_word(ds) = there ? v[0] : u32x4_t{0, 0, 0, 0};
     }
     bad |= (bool)__shfl_xor((int)bad, 32, 64);
     const unsigned long long bad_at = __ballot(there && bad);   // bit c: key tile_key(c)
     if (bad_at) {
 #pragma unroll
       for (int ds = 0; ds < DS; ++ds)
-        if (bad) s_vrow[ds] = u32x4_t{0, 0, 0, 0};
+        if (bad) v_word(ds) = u32x4_t{0, 0, 0, 0};
     }
     lds_written();
     f32x16_t s[QT];
@@ -500,7 +494,7 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
         for (int ds = 0; ds < DS; ++ds) {
           u32x4_t v[WP];
           load_planes<WP>((const T*)a.v + at + 8 * ds, 0, v);
-          s_vrow[ds] = there && !bad ? v[e] : u32x4_t{0, 0, 0, 0};
+          v_word(ds) = there && !bad ? v[e] : u32x4_t{0, 0, 0, 0};
         }
         lds_written();
       }
@@ -519,70 +513,83 @@ __global__ __launch_bounds__(64 * ATT_WAVES) void kv4_attention_kernel(const Kv4
     }
   }
 
-  // ---- the wavefronts' states into one, in a fixed order: the upper half of them deposits, the lower half adds, halved until one is left ----
-  constexpr int SLOT = 32 * D + 64;   // floats: output, maxima, sums
+  // ---- cached keys ----
+  if (!EARLY) first();
+  if (Q_LDS) {
+    size_t at = 0;
+    for (; tile < c1; tile += NW)
+      cached_tile(tile, kn, vn, [&]() __attribute__((always_inline)) {
+        if (tile + NW < c1) {
+          at = entry_of(tile + NW);
+          vn.load(vc, vs, at, h);
+          if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
+        }
+      }, [&]() __attribute__((always_inline)) {
+        if (tile + NW < c1) kn.load(kc, ks, at, h);
+      });
+  } else {
+    for (; tile < c1; tile += NW) {
+      const HalfRow<D> k = kn;
+      HalfRow<D> v = vn;
+      if (tile + NW < c1) {
+        request(tile + NW);
+        if (tile + 2 * NW < c1) request_page(tile + 2 * NW);
+      }
+      cached_tile(tile, k, v, []() {}, []() {});
+    }
+  }
+
+  // ---- the wavefronts' states into one: each deposits its own, every thread adds up four outputs of a row, in the order of the wavefronts ----
+  constexpr int SLOT = 32 * D + 64;   // floats: output in the accumulators' order, maxima, sums
   float* s_st = (float*)s_mem;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
+    if (t >= tiles_q) break;
     st[t].l += __shfl_xor(st[t].l, 32, 64);
-    for (int half = NW / 2; half > 0; half >>= 1) {
-      __syncthreads();
-      if (wave >= half && wave < 2 * half) {
-        float* p = s_st + (size_t)(wave - half) * SLOT;
+    __syncthreads();
+    float* p = s_st + (size_t)wave * SLOT;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            ((float4*)p)[(dt * 4 + i) * 64 + lane] = make_float4(st[t].o[dt][4 * i], st[t].o[dt][4 * i + 1], st[t].o[dt][4 * i + 2], st[t].o[dt][4 * i + 3]);
-        if (h == 0) { p[32 * D + c] = st[t].m; p[32 * D + 32 + c] = st[t].l; }
+      for (int i = 0; i < 4; ++i)
+        ((float4*)p)[(dt * 4 + i) * 64 + lane] = make_float4(st[t].o[dt][4 * i], st[t].o[dt][4 * i + 1], st[t].o[dt][4 * i + 2], st[t].o[dt][4 * i + 3]);
+    if (h == 0) { p[32 * D + c] = st[t].m; p[32 * D + 32 + c] = st[t].l; }
+    __syncthreads();
+    const int qi = q0 + t * 32 + c, head = kvh * a.grp + qi - a.group.div(min(qi, nq - 1)) * a.grp;
+    float m = s_st[32 * D + c], f[NW], l = 0.f;
+#pragma unroll
+    for (int k = 1; k < NW; ++k) m = fmaxf(m, s_st[k * SLOT + 32 * D + c]);
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      f[k] = __builtin_amdgcn_exp2f(s_st[k * SLOT + 32 * D + c] - m);
+      l += f[k] * s_st[k * SLOT + 32 * D + 32 + c];
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const size_t at = ((size_t)w * groups + qg) * QT + t;
+#pragma unroll
+    for (int g = wave; g < 4 * DT; g += NW) {
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        const float4 v = ((const float4*)(s_st + k * SLOT))[g * 64 + lane];
+        o.x += f[k] * v.x; o.y += f[k] * v.y; o.z += f[k] * v.z; o.w += f[k] * v.w;
       }
-      __syncthreads();
-      if (wave < half) {
-        const float* p = s_st + (size_t)wave * SLOT;
-        const float m2 = p[32 * D + c], l2 = p[32 * D + 32 + c], to = fmaxf(st[t].m, m2);
-        const float f1 = __builtin_amdgcn_exp2f(st[t].m - to), f2 = __builtin_amdgcn_exp2f(m2 - to);
-        st[t].m = to;
-        st[t].l = st[t].l * f1 + l2 * f2;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 v = ((const float4*)p)[(dt * 4 + i) * 64 + lane];
-            st[t].o[dt][4 * i] = st[t].o[dt][4 * i] * f1 + v.x * f2;
-            st[t].o[dt][4 * i + 1] = st[t].o[dt][4 * i + 1] * f1 + v.y * f2;
-            st[t].o[dt][4 * i + 2] = st[t].o[dt][4 * i + 2] * f1 + v.z * f2;
-            st[t].o[dt][4 * i + 3] = st[t].o[dt][4 * i + 3] * f1 + v.w * f2;
-          }
+      if (qi >= nq) continue;
+      if (it.splits > 1) {
+        ((float4*)(a.part_o + at * 32 * D))[g * 64 + lane] = o;
+      } else {
+        const int d = head * D + (g >> 2) * 32 + 8 * (g & 3) + 4 * h;
+        if (QM == Q_F32) *(float4*)((float*)a.out + row[t] * a.o_ld + d) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        else act_put4((bf16_t*)a.out, a.o_lo, row[t], d, (int)a.o_ld, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
       }
     }
-    if (wave == 0 && t < tiles_q) {
-      const int qi = q0 + t * 32 + c, head = kvh * a.grp + qi - a.group.div(min(qi, nq - 1)) * a.grp;
-      if (it.splits == 1) {
-        if (qi < nq) {
-          const float inv = st[t].l == 0.f ? 0.f : 1.f / st[t].l;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int d = head * D + dt * 32 + 8 * i + 4 * h;
-              const float x = st[t].o[dt][4 * i] * inv, y = st[t].o[dt][4 * i + 1] * inv, z = st[t].o[dt][4 * i + 2] * inv, u = st[t].o[dt][4 * i + 3] * inv;
-              if (QM == Q_F32) *(float4*)((float*)a.out + row[t] * a.o_ld + d) = make_float4(x, y, z, u);
-              else act_put4((bf16_t*)a.out, a.o_lo, row[t], d, (int)a.o_ld, x, y, z, u);
-            }
-          if (a.lse && h == 0) a.lse[(size_t)row[t] * a.Hq + head] = st[t].l == 0.f ? -INFINITY : (st[t].m + __builtin_amdgcn_logf(st[t].l)) * LN2;
-        }
-      } else if (qi < nq) {
-        // partial output in the accumulators' order, then maxima and sums; the first split says where the sequence's are
-        const size_t at = ((size_t)w * groups + qg) * QT + t;
-        float4* po = (float4*)(a.part_o + at * 32 * D);
-        if (t == 0 && qg == 0 && kvh == 0 && it.z == 0 && lane == 0) a.part_of[it.n] = make_int2(w / kv.H, it.splits);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            po[(dt * 4 + i) * 64 + lane] = make_float4(st[t].o[dt][4 * i], st[t].o[dt][4 * i + 1], st[t].o[dt][4 * i + 2], st[t].o[dt][4 * i + 3]);
-        if (h == 0) { a.part_ml[at * 64 + c] = st[t].m; a.part_ml[at * 64 + 32 + c] = st[t].l; }
-      }
+    if (wave == 0 && h == 0 && qi < nq) {
+      if (it.splits > 1) {
+        a.part_ml[at * 64 + c] = m;
+        a.part_ml[at * 64 + 32 + c] = l;
+        // the first split says where the sequence's are
+        if (t == 0 && qg == 0 && kvh == 0 && it.z == 0 && c == 0) a.part_of[it.n] = make_int2(w / kv.H, it.splits);
+      } else if (a.lse) a.lse[(size_t)row[t] * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
     }
   }
 }
@@ -600,7 +607,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int til
   if (qt * 32 >= nq || sq.tiles <= a.min_run) return;
   int total = 0;
   for (int n0 = tid & 63; n0 < a.N; n0 += 64) total += seq_tiles(a, n0).tiles;
-  if (sq.tiles <= run_of(a, __builtin_amdgcn_readfirstlane(wave_sum(total)))) return;
+  if (sq.tiles <= run_of(a, wave_sum(total))) return;
   if (qi >= nq) return;
   const int Z = of.y, groups = a.per_item / kv.H;
   const size_t step = (size_t)kv.H * groups * per_wg, at0 = (((size_t)of.x * kv.H + kvh) * groups + qt / per_wg) * per_wg + qt % per_wg;
@@ -769,7 +776,7 @@ static AttnShape shape_of(const Kv4& kv, int dtype, int planes, int N, int T, in
   s.groups = (s.q_tiles + s.per_wg - 1) / s.per_wg;
   const int per_item = kv.H * s.groups;
   // runs of the batch: at most the target, and one more a sequence; a sequence has no more than its pages hold
-  s.most = std::max(1, ((kv.cap + 31) / 32 + (window ? (T + 31) / 32 : 0) + MIN_RUN - 1) / MIN_RUN);
+  s.most = std::max(1, ((kv.cap + 31) / 32 + (window ? (T + 31) / 32 : 0) + min_run_of(kv.D) - 1) / min_run_of(kv.D));
   s.items = (int)std::min<long long>((long long)N * s.most, (TARGET + per_item - 1) / per_item + (long long)N);
   return s;
 }
@@ -786,13 +793,13 @@ size_t kv4_attention_bytes(const Kv4& kv, int N, int T, int Hq) {
 // Tiles of V and the queries, and after them the wavefronts' states.
 template <int D, int QT>
 static constexpr size_t attn_lds() {
-  return std::max((size_t)ATT_WAVES * 32 * V_LD<D> + (QT > 1 ? (size_t)QT * 32 * D * 2 : 0), (size_t)(ATT_WAVES / 2) * (32 * D + 64) * sizeof(float));
+  return std::max((size_t)waves_of(D) * 32 * V_LD<D> + (QT > 1 ? (size_t)QT * 32 * D * 2 : 0), (size_t)waves_of(D) * (32 * D + 64) * sizeof(float));
 }
 
 template <int D, int QM, int QT>
 static void launch_attn(hipStream_t st, const Kv4Attn& a, int layer, const AttnShape& s) {
   const int wgs = (a.items * a.kv.H + 7) / 8 * 8 * s.groups;
-  S2D2_LAUNCH((kv4_attention_kernel<D, QM, QT>), dim3(wgs), dim3(64 * ATT_WAVES), (attn_lds<D, QT>()), st, a, layer);
+  S2D2_LAUNCH((kv4_attention_kernel<D, QM, QT>), dim3(wgs), dim3(64 * waves_of(D)), (attn_lds<D, QT>()), st, a, layer);
   if (s.most > 1) S2D2_LAUNCH((kv4_merge_kernel<D, QM>), dim3(a.N * a.kv.H * s.q_tiles * (D / 32)), dim3(256), 0, st, a, s.q_tiles, s.per_wg);
 }
 
@@ -809,7 +816,7 @@ void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int
   a.items = s.items;
   a.per_item = a.kv.H * s.groups;
   a.target = TARGET;
-  a.min_run = MIN_RUN;
+  a.min_run = min_run_of(a.kv.D);
   const size_t slots = (size_t)((s.items * a.kv.H + 7) / 8 * 8) * s.groups * s.per_wg;
   a.part_o = (float*)scratch;
   a.part_ml = a.part_o + slots * 32 * a.kv.D;

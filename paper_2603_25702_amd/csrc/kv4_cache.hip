@@ -23,7 +23,7 @@ Kv4 kv4_of(const s2d2_kv4_view* view) {
 // by two DPP moves as an integer (the bits of |x| order as |x| does, with NaN above infinity above all else), v_cvt_scalef32_pk_fp4_f32
 // rounds x / 2^e to nearest-even codes.
 // ---------------------------------------------------------------------------------------------
-static constexpr int APPEND_ROWS = 4;   // rows of a sequence per workgroup
+static constexpr int APPEND_ROWS = 4;   // rows of a sequence per workgroup, all in flight at once
 
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
@@ -65,22 +65,32 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4 kv, Kv4Rows r, int 
   if (t0 >= rows || r.row0[n] > r.rows - rows || S + rows > kv.cap) return;   // (the commit flags a sequence without room)
   const int pos0 = kv.seq_len[n], units = kv.H * kv.D / 8, per_head = kv.D / 8;
   const int here = min(APPEND_ROWS, rows - t0);
-  const T* src[2] = {k + l * layer_stride + (r.row0[n] + t0) * row_stride, v + l * layer_stride + (r.row0[n] + t0) * row_stride};
-  for (int i = threadIdx.x; i < here * 2 * units; i += 256) {   // (a multiple of four: the lanes of a group stay together)
-    const int t = i / (2 * units), u = i % (2 * units), value = u >= units, w = u - value * units, head = w / per_head, part = w % per_head;
-    const int place = S + t0 + t, p = kv.ps.div(place);
-    const int page = kv.page_table[(size_t)n * kv.max_pages + p];
-    float x[8];
-    load8(src[value] + t * row_stride + (size_t)w * 8, x);
-    uint32_t scale;
-    const uint32_t codes = kv4_quantise(x, scale);
-    if (page < 0 || page >= kv.n_pages) continue;
-    const size_t at = l * kv.layer_entries + kv.at(page, head, place - p * kv.ps.d);
-    ((uint32_t*)((value ? kv.vc : kv.kc) + at * (kv.D / 2)))[part] = codes;
-    if ((part & 3) == 0) (value ? kv.vs : kv.ks)[at * (kv.D / 32) + part / 4] = (uint8_t)scale;
-    if (part == 0 && !value) {
-      if (kv.mass) kv.mass[at] = 0.f;
-      if (kv.position) kv.position[at] = pos0 + t0 + t;
+  const int64_t row = l * layer_stride + (int64_t)(r.row0[n] + t0) * row_stride;
+  int page[APPEND_ROWS], slot[APPEND_ROWS];
+#pragma unroll
+  for (int t = 0; t < APPEND_ROWS; ++t) {
+    const int place = S + t0 + min(t, here - 1), p = kv.ps.div(place);
+    page[t] = kv.page_table[(size_t)n * kv.max_pages + p];
+    slot[t] = place - p * kv.ps.d;
+  }
+  for (int i = threadIdx.x; i < 2 * units; i += 256) {   // (a multiple of four: the lanes of a group stay together)
+    const int value = i >= units, w = i - value * units, head = w / per_head, part = w % per_head;
+    const T* src = (value ? v : k) + row + (size_t)w * 8;
+    float x[APPEND_ROWS][8];
+#pragma unroll
+    for (int t = 0; t < APPEND_ROWS; ++t) load8(src + min(t, here - 1) * row_stride, x[t]);
+#pragma unroll
+    for (int t = 0; t < APPEND_ROWS; ++t) {
+      uint32_t scale;
+      const uint32_t codes = kv4_quantise(x[t], scale);
+      if (t >= here || page[t] < 0 || page[t] >= kv.n_pages) continue;
+      const size_t at = l * kv.layer_entries + kv.at(page[t], head, slot[t]);
+      ((uint32_t*)((value ? kv.vc : kv.kc) + at * (kv.D / 2)))[part] = codes;
+      if ((part & 3) == 0) (value ? kv.vs : kv.ks)[at * (kv.D / 32) + part / 4] = (uint8_t)scale;
+      if (part == 0 && !value) {
+        if (kv.mass) kv.mass[at] = 0.f;
+        if (kv.position) kv.position[at] = pos0 + t0 + t;
+      }
     }
   }
 }
@@ -109,39 +119,60 @@ void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv
 }
 
 // ---------------------------------------------------------------------------------------------
-// Entries read back: 8 values a thread.
+// Entries read back: 8 values a thread of each of READ_ROWS entries.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+static constexpr int READ_ROWS = 4;
 template <typename T>
-__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4 kv, int N, int T_, const int32_t* __restrict__ first, T* __restrict__ k, T* __restrict__ v) {
-  const int n = blockIdx.x / T_, t = blockIdx.x % T_, l = blockIdx.y;
-  const int64_t place = (int64_t)first[n] + t;
-  if (place < 0 || place >= kv.held(n)) return;
-  const int p = kv.ps.div((int)place), units = kv.H * kv.D / 8, per_head = kv.D / 8;
-  const int page = max(0, min(kv.page_table[(size_t)n * kv.max_pages + p], kv.n_pages - 1));
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4 kv, int N, int T_, int per_seq, const int32_t* __restrict__ first, T* __restrict__ k, T* __restrict__ v) {
+  const int n = blockIdx.x / per_seq, t0 = (blockIdx.x % per_seq) * READ_ROWS, l = blockIdx.y;
+  const int held = kv.held(n);
+  const int64_t place0 = (int64_t)first[n] + t0;
+  if (place0 >= held || place0 <= -READ_ROWS) return;
+  const int units = kv.H * kv.D / 8, per_head = kv.D / 8;
+  size_t entry[READ_ROWS];
+  bool there[READ_ROWS];
+#pragma unroll
+  for (int t = 0; t < READ_ROWS; ++t) {
+    const int64_t place = place0 + t;
+    there[t] = t0 + t < T_ && place >= 0 && place < held;
+    const int i = (int)max((int64_t)0, min(place, (int64_t)held - 1)), p = kv.ps.div(i);
+    entry[t] = l * kv.layer_entries + kv.at(max(0, min(kv.page_table[(size_t)n * kv.max_pages + p], kv.n_pages - 1)), 0, i - p * kv.ps.d);
+  }
   for (int i = threadIdx.x; i < 2 * units; i += 256) {
     const int value = i >= units, w = i - value * units, head = w / per_head, part = w % per_head;
-    const size_t at = l * kv.layer_entries + kv.at(page, head, (int)place - p * kv.ps.d);
-    const uint32_t c = ((const uint32_t*)((value ? kv.vc : kv.kc) + at * (kv.D / 2)))[part];
-    const float s = __int_as_float((int)(value ? kv.vs : kv.ks)[at * (kv.D / 32) + part / 4] << 23);   // (255: the conversion gives NaN)
-    const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
-    const f32x2_t d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
-    T* to = (value ? v : k) + (((size_t)l * N + n) * T_ + t) * kv.H * kv.D + (size_t)w * 8;
-    if (sizeof(T) == 2) {
-      // (exact: a code times a power of two has two significant bits)
-      auto two = [](f32x2_t x) { return (__float_as_uint(x[0]) >> 16) | (__float_as_uint(x[1]) & 0xffff0000u); };
-      *(uint4*)to = make_uint4(two(a), two(b), two(d), two(e));
-    } else {
-      ((float4*)to)[0] = make_float4(a[0], a[1], b[0], b[1]);
-      ((float4*)to)[1] = make_float4(d[0], d[1], e[0], e[1]);
+    const uint8_t *codes = value ? kv.vc : kv.kc, *scales = value ? kv.vs : kv.ks;
+    uint32_t c[READ_ROWS], e[READ_ROWS];
+#pragma unroll
+    for (int t = 0; t < READ_ROWS; ++t) {
+      const size_t at = entry[t] + (size_t)head * kv.ps.d;
+      c[t] = ((const uint32_t*)(codes + at * (kv.D / 2)))[part];
+      e[t] = scales[at * (kv.D / 32) + part / 4];
+    }
+#pragma unroll
+    for (int t = 0; t < READ_ROWS; ++t) {
+      if (!there[t]) continue;
+      const float s = __uint_as_float(e[t] << 23);   // (255: the conversion gives NaN)
+      const f32x2_t x[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[t], s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[t], s, 1),
+                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[t], s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[t], s, 3)};
+      T* to = (value ? v : k) + (((size_t)l * N + n) * T_ + t0 + t) * kv.H * kv.D + (size_t)w * 8;
+      if (sizeof(T) == 2) {
+        // (exact: a code times a power of two has two significant bits)
+        auto two = [](f32x2_t y) { return (__float_as_uint(y[0]) >> 16) | (__float_as_uint(y[1]) & 0xffff0000u); };
+        *(uint4*)to = make_uint4(two(x[0]), two(x[1]), two(x[2]), two(x[3]));
+      } else {
+        ((float4*)to)[0] = make_float4(x[0][0], x[0][1], x[1][0], x[1][1]);
+        ((float4*)to)[1] = make_float4(x[2][0], x[2][1], x[3][0], x[3][1]);
+      }
     }
   }
 }
 
 void launch_kv4_read(hipStream_t st, int dtype, const Kv4& kv, int N, int T, const int32_t* first, void* k, void* v) {
-  const dim3 grid(N * T, kv.n_layers);
-  if (dtype == S2D2_BF16) S2D2_LAUNCH(kv4_read_kernel<bf16_t>, grid, dim3(256), 0, st, kv, N, T, first, (bf16_t*)k, (bf16_t*)v);
-  else S2D2_LAUNCH(kv4_read_kernel<float>, grid, dim3(256), 0, st, kv, N, T, first, (float*)k, (float*)v);
+  const int per_seq = (T + READ_ROWS - 1) / READ_ROWS;
+  const dim3 grid(N * per_seq, kv.n_layers);
+  if (dtype == S2D2_BF16) S2D2_LAUNCH(kv4_read_kernel<bf16_t>, grid, dim3(256), 0, st, kv, N, T, per_seq, first, (bf16_t*)k, (bf16_t*)v);
+  else S2D2_LAUNCH(kv4_read_kernel<float>, grid, dim3(256), 0, st, kv, N, T, per_seq, first, (float*)k, (float*)v);
 }
 
 // ---------------------------------------------------------------------------------------------
