@@ -89,7 +89,8 @@ int32_t s2d2_kv4_read(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t 
 int64_t s2d2_kv4_attention_bytes(const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t n_q_heads);
 
 /* Attention of the windows over the entries of `layer` and over themselves.  scratch: device, 16-byte aligned, s2d2_kv4_attention_bytes() or
- * more; its contents do not matter and nothing is kept in it.  Calls that run at the same time need a scratch each.  N <= 1024, T <= 8192. */
+ * more; its contents do not matter and nothing is kept in it.  Calls that run at the same time need a scratch each.  N <= 1024, T <= 8192,
+ * N * (max_pages_per_seq * page_size + T + 64) below 2^36. */
 int32_t s2d2_kv4_attention(void* stream, const s2d2_kv4_view* kv, int32_t layer, const s2d2_kv4_rows* rows, void* scratch, size_t scratch_bytes);
 
 /* mass of every cached entry of `layer` and KV head += sum over the rows of its sequence's window and the query heads of the KV head of

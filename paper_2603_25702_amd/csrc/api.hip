@@ -430,7 +430,7 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
   // queries stay bf16 (the attention kernels multiply them with the cache's bf16 keys): hi + lo planes unless the
   // model asked for single bf16 planes; the kernel for wide windows takes them as half values in the half mode
   // (it converts the keys and values on their way into LDS)
-  const bool q_f16 = fused && wide && opm == OPM_F16;
+  const bool q_f16 = fused && (wide || kv4) && opm == OPM_F16;
   const int PQ = fused && (flash || kv4) && opm != OPM_BF16 && !q_f16 ? 2 : 1;
   const int ld_q = PQ * HqD, lo_q = q_f16 ? LO_F16 : (PQ == 2 ? HqD : 0);
   if (fused) { ProfScope ps(c, 3, 0.0); launch_embed_norm(st, c->w.embed, d.d_model, c->plan, R, c->layers[0].norm1, c->h, c->a, ld_a, lo_a, c->ss, ss_stride, c->rope_cs, d.head_dim, d.rope_theta); }
@@ -460,14 +460,15 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
     const void* kp = (const uint8_t*)kv->k_pages + l * page_layer;
     const void* vp = (const uint8_t*)kv->v_pages + l * page_layer;
     if (kv4) {
+      const int mode4 = dt == S2D2_F32 ? Q_F32 : q_f16 ? Q_F16 : PQ == 2 ? Q_BF16X2 : Q_BF16;
       Kv4Attn x{};
-      x.kv = c->kv4; x.N = N; x.T = sz.win; x.rows = R; x.Hq = d.n_q_heads; x.grp = d.n_q_heads / d.n_kv_heads; x.group = divisor_of(x.grp);
-      x.q = c->qbuf; x.q_ld = fused ? ld_q : HqD; x.q_lo = lo_q; x.k = kw; x.v = vw; x.kv_ld = (int64_t)d.n_kv_heads * d.head_dim;
+      x.kv = c->kv4; x.N = N; x.T = sz.win; x.expect = (sz.hint + N - 1) / N; x.rows = R; x.Hq = d.n_q_heads; x.grp = d.n_q_heads / d.n_kv_heads; x.group = divisor_of(x.grp);
+      x.q = c->qbuf; x.q_ld = fused ? ld_q : HqD; x.q_lo = q_f16 ? 0 : lo_q; x.k = q_f16 ? c->kwin16 : kw; x.v = vw; x.kv_ld = (int64_t)d.n_kv_heads * d.head_dim;
       x.row0 = c->plan.seq_row0; x.n_rows = c->plan.seq_rows; x.lo = c->plan.row_lo; x.hi = c->plan.row_hi;
       x.out = c->obuf; x.o_ld = ld_o; x.o_lo = lo_o; x.lse = weigh ? c->kv4_lse : nullptr;
       x.scale_log2e = 1.44269504088896340736f / sqrtf((float)d.head_dim);
-      { ProfScope ps(c, 1, 0.0); launch_kv4_attention(st, dt, PQ, x, l, c->kv4_scratch); }
-      if (weigh) { ProfScope ps(c, 1, 0.0); launch_kv4_weigh(st, dt, PQ, x, l); }
+      { ProfScope ps(c, 1, 0.0); launch_kv4_attention(st, mode4, x, l, c->kv4_scratch); }
+      if (weigh) { ProfScope ps(c, 1, 0.0); launch_kv4_weigh(st, mode4, x, l); }
       if (LR == 0 && l == d.n_layers - 1) return check_launch("forward");
     } else if (wide) {
       { ProfScope ps(c, 1, 0.0); launch_attention_wide(st, c->qbuf, fused ? ld_q : HqD, fused ? lo_q : 0, q_f16 ? c->kwin16 : kw, c->vT_win, kp, vp, g, c->plan, N, d.n_q_heads, q_tiles, ws.per, ws.nw, Z, ws.target, ws.tiles, c->n_cus, c->wpad, c->obuf, ld_o, lo_o, c->attn_part, c->attn_part_entries); }

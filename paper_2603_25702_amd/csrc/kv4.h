@@ -57,17 +57,21 @@ struct Kv4Attn {
   float scale_log2e;   // scores to base 2
   float *part_o, *part_ml;
   int2* part_of;     // [N] of a sequence with several splits: its first item, its splits
+  int32_t expect;    // rows that a sequence is expected to have (at most T): what the splits are chosen for
+  int32_t groups;    // groups of query tiles of T rows
   int32_t items;     // (sequence, split) pairs the grid holds
-  int32_t per_item;  // workgroups of one: KV heads * groups of query tiles
+  int32_t per_item;  // workgroups of one with the expected rows: KV heads * groups of query tiles
+  int32_t room;      // splits beyond one a sequence that the scratch holds
   int32_t target;    // workgroups to aim for
   int32_t min_run;   // tiles of a split, at least
   Divisor group;     // by query heads per KV head
 };
 
-// dtype of the queries, window rows and output: S2D2_BF16 / S2D2_F32; planes 2: bf16 queries in two planes
-void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int layer, void* scratch);
+// Queries and window rows: bf16; bf16 queries in two planes; queries and window keys as half values; fp32
+enum Kv4Query { Q_BF16 = 0, Q_BF16X2 = 1, Q_F16 = 2, Q_F32 = 3 };
+void launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void* scratch);
 size_t kv4_attention_bytes(const Kv4& kv, int N, int T, int Hq);
-void launch_kv4_weigh(hipStream_t st, int dtype, int planes, Kv4Attn& a, int layer);
+void launch_kv4_weigh(hipStream_t st, int mode, Kv4Attn& a, int layer);
 int kv4_evict_init();
 int kv4_attention_init();
 

@@ -52,6 +52,11 @@ int32_t check_q_heads(const s2d2_kv4_view* kv, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads > 1024 || n_q_heads % kv->n_kv_heads) return fail(S2D2_EINVAL, "n_q_heads=%d must be a positive multiple of n_kv_heads=%d, at most 1024", n_q_heads, kv->n_kv_heads);
   return S2D2_OK;
 }
+// Key tiles of a batch are counted in 31 bits.
+int32_t check_keys(const s2d2_kv4_view* kv, int32_t N, int32_t T) {
+  if (((int64_t)kv->max_pages_per_seq * kv->page_size + T + 64) * N >= (1ll << 36)) return fail(S2D2_EINVAL, "N=%d sequences of up to %lld keys are too many for one call", N, (long long)kv->max_pages_per_seq * kv->page_size + T);
+  return S2D2_OK;
+}
 // A row stride in elements: whole 16 bytes, at least a row, and offsets of all rows in 63 bits
 bool stride_ok(int64_t stride, int64_t width, int32_t dtype) { return stride >= width && stride < (1ll << 31) && stride % (dtype == S2D2_F32 ? 4 : 8) == 0; }
 
@@ -60,7 +65,7 @@ int32_t attn_args(const s2d2_kv4_view* kv, int32_t layer, const s2d2_kv4_rows* r
   if ((rc = check_kv4(kv))) return rc;
   if (layer < 0 || layer >= kv->n_layers) return fail(S2D2_EINVAL, "layer=%d outside [0, n_layers=%d)", layer, kv->n_layers);
   if (!r) return fail(S2D2_EINVAL, "rows are NULL");
-  if ((rc = check_batch(r->N, r->T, 8192)) || (rc = check_dtype(r->dtype)) || (rc = check_q_heads(kv, r->n_q_heads))) return rc;
+  if ((rc = check_batch(r->N, r->T, 8192)) || (rc = check_dtype(r->dtype)) || (rc = check_q_heads(kv, r->n_q_heads)) || (rc = check_keys(kv, r->N, r->T))) return rc;
   if (r->rows < 1) return fail(S2D2_EINVAL, "rows=%d must be positive", r->rows);
   if (!(r->scale > 0.f) || r->scale > 3e38f) return fail(S2D2_EINVAL, "scale must be positive and finite");
   if (!r->q || !r->row0 || !r->n_rows) return fail(S2D2_EINVAL, "q, row0 or n_rows is NULL");
@@ -76,7 +81,7 @@ int32_t attn_args(const s2d2_kv4_view* kv, int32_t layer, const s2d2_kv4_rows* r
   }
   a = Kv4Attn{};
   a.kv = kv4_of(kv);
-  a.N = r->N; a.T = r->T; a.rows = r->rows; a.Hq = r->n_q_heads; a.grp = r->n_q_heads / kv->n_kv_heads;
+  a.N = r->N; a.T = a.expect = r->T; a.rows = r->rows; a.Hq = r->n_q_heads; a.grp = r->n_q_heads / kv->n_kv_heads;
   a.q = r->q; a.q_ld = r->q_stride; a.row0 = r->row0; a.n_rows = r->n_rows; a.lse = r->lse;
   a.group = divisor_of(a.grp);
   a.scale_log2e = r->scale * 1.44269504088896340736f;
@@ -114,7 +119,7 @@ int32_t s2d2_kv4_read(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t 
 
 int64_t s2d2_kv4_attention_bytes(const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t n_q_heads) {
   int32_t rc;
-  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 8192)) || (rc = check_q_heads(kv, n_q_heads))) return rc;
+  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 8192)) || (rc = check_q_heads(kv, n_q_heads)) || (rc = check_keys(kv, N, T))) return rc;
   return (int64_t)kv4_attention_bytes(kv4_of(kv), N, T, n_q_heads);
 }
 
@@ -126,7 +131,7 @@ int32_t s2d2_kv4_attention(void* stream, const s2d2_kv4_view* kv, int32_t layer,
   if (scratch_bytes < need) return fail(S2D2_ENOSPC, "scratch has %zu bytes, %zu needed", scratch_bytes, need);
   if (need && (!scratch || ((uintptr_t)scratch & 15))) return fail(S2D2_EINVAL, "scratch is NULL or not 16-byte aligned");
   if ((rc = kv4_ready())) return rc;
-  launch_kv4_attention((hipStream_t)stream, rows->dtype, 1, a, layer, scratch);
+  launch_kv4_attention((hipStream_t)stream, rows->dtype == S2D2_F32 ? Q_F32 : Q_BF16, a, layer, scratch);
   return check_launch("s2d2_kv4_attention");
 }
 
@@ -134,7 +139,7 @@ int32_t s2d2_kv4_weigh(void* stream, const s2d2_kv4_view* kv, int32_t layer, con
   Kv4Attn a;
   int32_t rc;
   if ((rc = attn_args(kv, layer, rows, true, a)) || (rc = kv4_ready())) return rc;
-  launch_kv4_weigh((hipStream_t)stream, rows->dtype, 1, a, layer);
+  launch_kv4_weigh((hipStream_t)stream, rows->dtype == S2D2_F32 ? Q_F32 : Q_BF16, a, layer);
   return check_launch("s2d2_kv4_weigh");
 }
 

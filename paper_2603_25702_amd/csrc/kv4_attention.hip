@@ -35,11 +35,11 @@ static constexpr float MOST = 32768.f;              // and moves when the weight
 constexpr int waves_of(int D) { return D == 256 ? 4 : 8; }
 constexpr int min_run_of(int D) { return 4 * waves_of(D); }   // tiles of a split, at least: four a wavefront
 
-enum QueryMode { Q_BF16 = 0, Q_BF16X2 = 1, Q_F32 = 2 };
 template <int QM> struct Mode;
 // QP: planes of the queries; PP: of the softmax weights on cached values (half); WP: of the window's keys and values; WPP: of the weights on them (bf16)
 template <> struct Mode<Q_BF16> { typedef bf16_t T; static constexpr int QP = 1, PP = 1, WP = 1, WPP = 2; };
 template <> struct Mode<Q_BF16X2> { typedef bf16_t T; static constexpr int QP = 2, PP = 1, WP = 1, WPP = 2; };
+template <> struct Mode<Q_F16> { typedef bf16_t T; static constexpr int QP = 1, PP = 1, WP = 1, WPP = 2; };
 template <> struct Mode<Q_F32> { typedef float T; static constexpr int QP = 3, PP = 2, WP = 3, WPP = 3; };
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
@@ -76,6 +76,12 @@ __device__ __forceinline__ u32x4_t codes_f16(uint32_t w, float s) {
   r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
   return r;
 }
+
+// 8 codes and the product with queries in a mode's operand type
+template <int QM>
+__device__ __forceinline__ u32x4_t codes_for(uint32_t w, float s) { return QM == Q_F16 ? codes_f16(w, s) : codes_bf16(w, s); }
+template <int QM>
+__device__ __forceinline__ f32x16_t score_mfma(const u32x4_t& a, const u32x4_t& b, const f32x16_t& c) { return QM == Q_F16 ? mfma_f16(a, b, c) : mfma_bf16(a, b, c); }
 
 // 8 values as P planes of bf16 whose sum is the value (P = 3: exactly, above the subnormals)
 template <int P>
@@ -138,7 +144,8 @@ __device__ __forceinline__ int splits_of_seq(const SeqTiles& s, int run) { retur
 // so that a long sequence among many short ones is still split.
 __device__ __forceinline__ int run_of(const Kv4Attn& a, int total) {
   const long long wanted = 2ll * total * a.per_item, over = max(2ll * a.target - (long long)a.N * a.per_item, 4ll * a.target / 3);
-  return max(a.min_run, (int)((wanted + over - 1) / over));
+  const int fits = a.room > 0 ? (total + a.room - 1) / a.room : 1 << 30;   // (the scratch holds them)
+  return max(max(a.min_run, fits), (int)((wanted + over - 1) / over));
 }
 
 // The sequence and split of item w; false: there is none.  All lanes of the wavefront, the same answer in each.
@@ -260,9 +267,8 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
   extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
   const Kv4& kv = a.kv;
-  // workgroups of one run of keys lie 8 apart: on one XCD, whose cache they share
-  const int groups = a.per_item / kv.H, wg = blockIdx.x;
-  const int qg = (wg >> 3) % groups, w = ((wg >> 3) / groups) * 8 + (wg & 7), kvh = w % kv.H;
+  // The workgroups of one run of keys lie a multiple of 8 apart: on one XCD, whose cache they share.  Groups of rows that fewer sequences have come last.
+  const int groups = a.groups, per_group = gridDim.x / groups, qg = blockIdx.x / per_group, w = blockIdx.x % per_group, kvh = w % kv.H;
   Item it;
   if (!find_item(a, w / kv.H, lane, it)) return;
   const SeqTiles& sq = it.s;
@@ -369,12 +375,12 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
       for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
 #pragma unroll
     for (int ds = 0; ds < DS; ++ds) {
-      const u32x4_t kf = codes_bf16(k.w[ds], k.scale(ds));
+      const u32x4_t kf = codes_for<QM>(k.w[ds], k.scale(ds));
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int p = 0; p < QP; ++p) {
-          s[t] = mfma_bf16(kf, Q_LDS ? qa[ds % AHEAD][t][p] : query(t, ds, p), s[t]);
+          s[t] = score_mfma<QM>(kf, Q_LDS ? qa[ds % AHEAD][t][p] : query(t, ds, p), s[t]);
           if (Q_LDS && ds + AHEAD < DS) qa[ds % AHEAD][t][p] = query(t, ds + AHEAD, p);
         }
       if (Q_LDS) __builtin_amdgcn_sched_barrier(0);
@@ -467,7 +473,7 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
         for (int e = 0; e < WP; ++e)
 #pragma unroll
           for (int p = 0; p < QP; ++p)
-            if (e + p < (QP > WP ? QP : WP)) s[t] = mfma_bf16(kf[e], query(t, ds, p), s[t]);
+            if (e + p < (QP > WP ? QP : WP)) s[t] = score_mfma<QM>(kf[e], query(t, ds, p), s[t]);
     }
     u32x4_t pw[QT][2][WPP];
 #pragma unroll
@@ -609,7 +615,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int til
   for (int n0 = tid & 63; n0 < a.N; n0 += 64) total += seq_tiles(a, n0).tiles;
   if (sq.tiles <= run_of(a, wave_sum(total))) return;
   if (qi >= nq) return;
-  const int Z = of.y, groups = a.per_item / kv.H;
+  const int Z = of.y, groups = a.groups;
   const size_t step = (size_t)kv.H * groups * per_wg, at0 = (((size_t)of.x * kv.H + kvh) * groups + qt / per_wg) * per_wg + qt % per_wg;
   const float* ml = a.part_ml + at0 * 64 + c;
   const float4* po = (const float4*)(a.part_o + at0 * 32 * D) + (dt * 4 + g) * 64 + 32 * h + c;
@@ -712,7 +718,7 @@ __global__ __launch_bounds__(64 * WEIGH_WAVES, D <= 128 ? 3 : 2) void kv4_weigh_
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int ds = 0; ds < DS; ++ds) kf[x][ds] = codes_bf16(next[x].w[ds], next[x].scale(ds));
+        for (int ds = 0; ds < DS; ++ds) kf[x][ds] = codes_for<QM>(next[x].w[ds], next[x].scale(ds));
       if (tile + 2 * NW < t1) request(tile + 2 * NW);
       float sum[2] = {0.f, 0.f};
       for (int t = 0; t < tiles; ++t) {
@@ -727,7 +733,7 @@ __global__ __launch_bounds__(64 * WEIGH_WAVES, D <= 128 ? 3 : 2) void kv4_weigh_
           for (int e = 0; e < QP; ++e) {
             const u32x4_t qf = s_q[((t * DS + ds) * QP + e) * 64 + lane];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) s[x] = mfma_bf16(qf, kf[x][ds], s[x]);
+            for (int x = 0; x < 2; ++x) s[x] = score_mfma<QM>(qf, kf[x][ds], s[x]);
           }
         float ref[16];   // of rows 8 (i / 4) + 4 h + i % 4
 #pragma unroll
@@ -766,28 +772,30 @@ static constexpr int WEIGH_TARGET = 768, WEIGH_MIN_RUN = 16;   // three workgrou
 static constexpr int TARGET = 256;   // workgroups that are resident at once: one a compute unit (eight wavefronts of up to 256 registers)
 
 // Query tiles per workgroup: two share the conversion of K and V; one where there is no second, and where two would not leave registers.
-static int tiles_per_wg(int D, int dtype, int planes, int q_tiles) { return D <= 128 && dtype == S2D2_BF16 && planes == 1 && q_tiles >= 2 ? 2 : 1; }
+static int tiles_per_wg(int D, int mode, int q_tiles) { return D <= 128 && (mode == Q_BF16 || mode == Q_F16) && q_tiles >= 2 ? 2 : 1; }
 
-struct AttnShape { int q_tiles, per_wg, groups, items, most; };
-static AttnShape shape_of(const Kv4& kv, int dtype, int planes, int N, int T, int Hq, bool window) {
+struct AttnShape { int q_tiles, per_wg, groups, per_item, items, most, room; };
+// Slots of partial results that the scratch holds: those of four times the resident workgroups (a launch for fewer rows than T allows has more
+// splits than one for T rows), and of one run a sequence, KV head and query tile, with what rounding up adds.  Grows with N and T.
+static size_t slots_of(const Kv4& kv, int N, int q_tiles) { return 4 * TARGET + ((size_t)(N + 1) * kv.H + 8) * (q_tiles + 1); }
+static AttnShape shape_of(const Kv4& kv, int mode, int N, int T, int expect, int Hq, bool window) {
   AttnShape s;
   s.q_tiles = (T * (Hq / kv.H) + 31) / 32;
-  s.per_wg = tiles_per_wg(kv.D, dtype, planes, s.q_tiles);
+  s.per_wg = tiles_per_wg(kv.D, mode, s.q_tiles);
   s.groups = (s.q_tiles + s.per_wg - 1) / s.per_wg;
-  const int per_item = kv.H * s.groups;
-  // runs of the batch: at most the target, and one more a sequence; a sequence has no more than its pages hold
+  const int expected = (std::min(expect, T) * (Hq / kv.H) + 31) / 32;
+  s.per_item = kv.H * ((expected + s.per_wg - 1) / s.per_wg);
+  // runs of the batch: at most the target, and one more a sequence, what the scratch holds; a sequence has no more than its pages hold
+  s.room = (int)((slots_of(kv, N, s.q_tiles) / (s.groups * s.per_wg) - 8) / kv.H) - N;
   s.most = std::max(1, ((kv.cap + 31) / 32 + (window ? (T + 31) / 32 : 0) + min_run_of(kv.D) - 1) / min_run_of(kv.D));
-  s.items = (int)std::min<long long>((long long)N * s.most, (TARGET + per_item - 1) / per_item + (long long)N);
+  s.items = (int)std::min<long long>((long long)N * s.most, std::max(0, std::min((TARGET + s.per_item - 1) / s.per_item, s.room)) + (long long)N);
   return s;
 }
 
-// Enough for every smaller N and T as well: the target's workgroups, with two query tiles each at most, and one run a sequence, KV head and tile,
-// with what rounding up adds.
 size_t kv4_attention_bytes(const Kv4& kv, int N, int T, int Hq) {
-  const AttnShape s = shape_of(kv, S2D2_BF16, 1, N, T, Hq, true);
+  const AttnShape s = shape_of(kv, Q_BF16, N, T, T, Hq, true);
   if (s.most < 2) return 0;
-  const size_t slots = 2 * TARGET + ((size_t)(N + 1) * kv.H + 8) * (s.q_tiles + 1);
-  return ((slots * (32 * kv.D + 64) + 2 * N) * sizeof(float) + 255) & ~(size_t)255;
+  return ((slots_of(kv, N, s.q_tiles) * (32 * kv.D + 64) + 2 * N) * sizeof(float) + 255) & ~(size_t)255;
 }
 
 // Tiles of V and the queries, and after them the wavefronts' states.
@@ -811,10 +819,12 @@ static void by_head_dim(int D, const F& f) {
   else f(std::integral_constant<int, 256>{});
 }
 
-void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int layer, void* scratch) {
-  const AttnShape s = shape_of(a.kv, dtype, planes, a.N, a.T, a.Hq, a.k != nullptr);
+void launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void* scratch) {
+  const AttnShape s = shape_of(a.kv, mode, a.N, a.T, a.expect, a.Hq, a.k != nullptr);
   a.items = s.items;
-  a.per_item = a.kv.H * s.groups;
+  a.per_item = s.per_item;
+  a.groups = s.groups;
+  a.room = s.room;
   a.target = TARGET;
   a.min_run = min_run_of(a.kv.D);
   const size_t slots = (size_t)((s.items * a.kv.H + 7) / 8 * 8) * s.groups * s.per_wg;
@@ -823,16 +833,20 @@ void launch_kv4_attention(hipStream_t st, int dtype, int planes, Kv4Attn& a, int
   a.part_of = (int2*)(a.part_ml + slots * 64);
   by_head_dim(a.kv.D, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    if (dtype == S2D2_F32) launch_attn<D, Q_F32, 1>(st, a, layer, s);
-    else if (planes == 2) launch_attn<D, Q_BF16X2, 1>(st, a, layer, s);
-    else if (D <= 128 && s.per_wg == 2) launch_attn<(D <= 128 ? D : 128), Q_BF16, 2>(st, a, layer, s);
+    constexpr int D2 = D <= 128 ? D : 128;
+    if (mode == Q_F32) launch_attn<D, Q_F32, 1>(st, a, layer, s);
+    else if (mode == Q_BF16X2) launch_attn<D, Q_BF16X2, 1>(st, a, layer, s);
+    else if (mode == Q_F16 && s.per_wg == 2) launch_attn<D2, Q_F16, 2>(st, a, layer, s);
+    else if (mode == Q_F16) launch_attn<D, Q_F16, 1>(st, a, layer, s);
+    else if (s.per_wg == 2) launch_attn<D2, Q_BF16, 2>(st, a, layer, s);
     else launch_attn<D, Q_BF16, 1>(st, a, layer, s);
   });
 }
 
-void launch_kv4_weigh(hipStream_t st, int dtype, int planes, Kv4Attn& a, int layer) {
+void launch_kv4_weigh(hipStream_t st, int mode, Kv4Attn& a, int layer) {
   a.k = a.v = nullptr;
   a.per_item = a.kv.H;
+  a.room = 1 << 30;
   a.target = WEIGH_TARGET;
   a.min_run = WEIGH_MIN_RUN;
   const int most = std::max(1, ((a.kv.cap + 31) / 32 + WEIGH_MIN_RUN - 1) / WEIGH_MIN_RUN);
@@ -840,8 +854,9 @@ void launch_kv4_weigh(hipStream_t st, int dtype, int planes, Kv4Attn& a, int lay
   by_head_dim(a.kv.D, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     const dim3 grid(a.items * a.kv.H), wg(64 * WEIGH_WAVES);
-    if (dtype == S2D2_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32>), grid, wg, (weigh_lds<D, Q_F32>()), st, a, layer);
-    else if (planes == 2) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16X2>), grid, wg, (weigh_lds<D, Q_BF16X2>()), st, a, layer);
+    if (mode == Q_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32>), grid, wg, (weigh_lds<D, Q_F32>()), st, a, layer);
+    else if (mode == Q_BF16X2) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16X2>), grid, wg, (weigh_lds<D, Q_BF16X2>()), st, a, layer);
+    else if (mode == Q_F16) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F16>), grid, wg, (weigh_lds<D, Q_F16>()), st, a, layer);
     else S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16>), grid, wg, (weigh_lds<D, Q_BF16>()), st, a, layer);
   });
 }
@@ -856,10 +871,14 @@ int kv4_attention_init() {
       limit((const void*)kv4_attention_kernel<D, Q_BF16, 1>, attn_lds<D, 1>());
       limit((const void*)kv4_attention_kernel<D, Q_BF16X2, 1>, attn_lds<D, 1>());
       limit((const void*)kv4_attention_kernel<D, Q_F32, 1>, attn_lds<D, 1>());
+      limit((const void*)kv4_attention_kernel<D, Q_F16, 1>, attn_lds<D, 1>());
+      limit((const void*)kv4_weigh_kernel<D, Q_F16>, weigh_lds<D, Q_F16>());
       limit((const void*)kv4_weigh_kernel<D, Q_BF16>, weigh_lds<D, Q_BF16>());
       limit((const void*)kv4_weigh_kernel<D, Q_BF16X2>, weigh_lds<D, Q_BF16X2>());
       limit((const void*)kv4_weigh_kernel<D, Q_F32>, weigh_lds<D, Q_F32>());
-      if (D <= 128) limit((const void*)kv4_attention_kernel<(D <= 128 ? D : 128), Q_BF16, 2>, attn_lds<(D <= 128 ? D : 128), 2>());
+      constexpr int D2 = D <= 128 ? D : 128;
+      limit((const void*)kv4_attention_kernel<D2, Q_BF16, 2>, attn_lds<D2, 2>());
+      limit((const void*)kv4_attention_kernel<D2, Q_F16, 2>, attn_lds<D2, 2>());
     });
   return e == hipSuccess ? 0 : -1;
 }

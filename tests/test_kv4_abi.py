@@ -92,6 +92,9 @@ def test_other_refusals(lib):
         assert lib.s2d2_kv4_attention(None, w, layer, rows(), FAKE, 1 << 40) == EINVAL
         assert lib.s2d2_kv4_weigh(None, w, layer, rows()) == EINVAL
     assert lib.s2d2_kv4_attention(None, w, 0, None, FAKE, 1 << 40) == EINVAL
+    huge = view(max_pages_per_seq=(1 << 26) - 1)
+    assert lib.s2d2_kv4_attention_bytes(huge, 63, 8, 32) > 0 and lib.s2d2_kv4_attention_bytes(huge, 64, 8, 32) == EINVAL   # 64 * (2^30 - 16 + 8 + 64) >= 2^36
+    assert lib.s2d2_kv4_weigh(None, huge, 0, rows(N=100)) == EINVAL and lib.s2d2_kv4_attention(None, huge, 0, rows(N=100), FAKE, 1 << 60) == EINVAL
     big = view(max_pages_per_seq=1024)
     need = lib.s2d2_kv4_attention_bytes(big, 4, 8, 32)
     assert need > 0
