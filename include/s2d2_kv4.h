@@ -77,7 +77,7 @@ typedef struct {
 /* Rows n_rows[n] (values outside [0, T] are cut) of k, v [n_layers, rows, n_kv_heads, head_dim] in `dtype` from row row0[n] on, layer_stride and
  * row_stride elements apart (16-byte aligned, strides whole 16 bytes), become entries of all layers behind those of sequence n;
  * entries[n] and seq_len[n] advance.  mass of a new entry: 0; position: seq_len[n] + i.  Without room for all of them nothing of that
- * sequence is written and status[n] is set to S2D2_ENOSPC.  A sequence whose rows leave [0, rows) is skipped.  N <= 1024. */
+ * sequence is written and status[n] is set to S2D2_ENOSPC.  A sequence whose rows leave [0, rows) is skipped.  N <= 1024, N * T below 2^26. */
 int32_t s2d2_kv4_append(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t rows, int32_t dtype, const void* k, const void* v,
                         int64_t layer_stride, int64_t row_stride, const int32_t* row0, const int32_t* n_rows);
 
@@ -90,7 +90,7 @@ int64_t s2d2_kv4_attention_bytes(const s2d2_kv4_view* kv, int32_t N, int32_t T, 
 
 /* Attention of the windows over the entries of `layer` and over themselves.  scratch: device, 16-byte aligned, s2d2_kv4_attention_bytes() or
  * more; its contents do not matter and nothing is kept in it.  Calls that run at the same time need a scratch each.  N <= 1024, T <= 8192,
- * N * (max_pages_per_seq * page_size + T + 64) below 2^36. */
+ * N * (max_pages_per_seq * page_size + T + 64) below 2^36, N * T * n_q_heads at most 2^25. */
 int32_t s2d2_kv4_attention(void* stream, const s2d2_kv4_view* kv, int32_t layer, const s2d2_kv4_rows* rows, void* scratch, size_t scratch_bytes);
 
 /* mass of every cached entry of `layer` and KV head += sum over the rows of its sequence's window and the query heads of the KV head of
@@ -102,7 +102,7 @@ int32_t s2d2_kv4_weigh(void* stream, const s2d2_kv4_view* kv, int32_t layer, con
  * first `sink` positions (position < sink) and of the last `recent` (position >= seq_len[n] - recent), then those of the largest mass; ties: the
  * lower entry first; a NaN counts as less than any other mass.  The i-th entry below `budget` that goes is replaced by the i-th one from `budget` on that stays
  * (codes, scales, mass and position as they are); all others stay where they are.  entries[n] becomes budget.  Needs mass and position;
- * budget >= 1, slack >= 0, sink + recent <= budget.  N <= 1024.  scratch: device, 4-byte aligned, s2d2_kv4_evict_bytes() or more; its contents do not
+ * budget >= 1, slack >= 0, sink + recent <= budget.  N <= 1024, N * n_layers * n_kv_heads below 2^22.  scratch: device, 4-byte aligned, s2d2_kv4_evict_bytes() or more; its contents do not
  * matter and nothing is kept in it.  Calls that run at the same time need a scratch (and a cache) each. */
 int32_t s2d2_kv4_evict(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t budget, int32_t slack, int32_t sink, int32_t recent, void* scratch,
                        size_t scratch_bytes);

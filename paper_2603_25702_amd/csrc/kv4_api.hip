@@ -48,12 +48,21 @@ int32_t check_batch(int32_t N, int32_t T, int32_t most) {
   if (T < 1 || T > most) return fail(S2D2_EINVAL, "T=%d outside [1, %d]", T, most);
   return S2D2_OK;
 }
+int32_t check_rows(int32_t N, int32_t T) {
+  if (((int64_t)T + 3) / 4 * N >= 1 << 24) return fail(S2D2_EINVAL, "N=%d sequences of up to T=%d rows are too many for one call", N, T);
+  return S2D2_OK;
+}
+int32_t check_lists(const s2d2_kv4_view* kv, int32_t N) {
+  if ((int64_t)N * kv->n_layers * kv->n_kv_heads >= 1 << 22) return fail(S2D2_EINVAL, "N * n_layers * n_kv_heads must be below 2^22");
+  return S2D2_OK;
+}
 int32_t check_q_heads(const s2d2_kv4_view* kv, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads > 1024 || n_q_heads % kv->n_kv_heads) return fail(S2D2_EINVAL, "n_q_heads=%d must be a positive multiple of n_kv_heads=%d, at most 1024", n_q_heads, kv->n_kv_heads);
   return S2D2_OK;
 }
-// Key tiles of a batch are counted in 31 bits.
-int32_t check_keys(const s2d2_kv4_view* kv, int32_t N, int32_t T) {
+// Key tiles of a batch are counted in 31 bits; a launch has less than 2^32 threads a dimension.
+int32_t check_keys(const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t n_q_heads) {
+  if ((int64_t)N * T * n_q_heads > 1 << 25) return fail(S2D2_EINVAL, "N * T * n_q_heads = %lld above 2^25", (long long)N * T * n_q_heads);
   if (((int64_t)kv->max_pages_per_seq * kv->page_size + T + 64) * N >= (1ll << 36)) return fail(S2D2_EINVAL, "N=%d sequences of up to %lld keys are too many for one call", N, (long long)kv->max_pages_per_seq * kv->page_size + T);
   return S2D2_OK;
 }
@@ -65,7 +74,7 @@ int32_t attn_args(const s2d2_kv4_view* kv, int32_t layer, const s2d2_kv4_rows* r
   if ((rc = check_kv4(kv))) return rc;
   if (layer < 0 || layer >= kv->n_layers) return fail(S2D2_EINVAL, "layer=%d outside [0, n_layers=%d)", layer, kv->n_layers);
   if (!r) return fail(S2D2_EINVAL, "rows are NULL");
-  if ((rc = check_batch(r->N, r->T, 8192)) || (rc = check_dtype(r->dtype)) || (rc = check_q_heads(kv, r->n_q_heads)) || (rc = check_keys(kv, r->N, r->T))) return rc;
+  if ((rc = check_batch(r->N, r->T, 8192)) || (rc = check_dtype(r->dtype)) || (rc = check_q_heads(kv, r->n_q_heads)) || (rc = check_keys(kv, r->N, r->T, r->n_q_heads))) return rc;
   if (r->rows < 1) return fail(S2D2_EINVAL, "rows=%d must be positive", r->rows);
   if (!(r->scale > 0.f) || r->scale > 3e38f) return fail(S2D2_EINVAL, "scale must be positive and finite");
   if (!r->q || !r->row0 || !r->n_rows) return fail(S2D2_EINVAL, "q, row0 or n_rows is NULL");
@@ -96,7 +105,7 @@ extern "C" {
 int32_t s2d2_kv4_append(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t rows, int32_t dtype, const void* k, const void* v,
                         int64_t layer_stride, int64_t row_stride, const int32_t* row0, const int32_t* n_rows) {
   int32_t rc;
-  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 1 << 20)) || (rc = check_dtype(dtype))) return rc;
+  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 1 << 20)) || (rc = check_rows(N, T)) || (rc = check_dtype(dtype))) return rc;
   if (rows < 1) return fail(S2D2_EINVAL, "rows=%d must be positive", rows);
   if (!k || !v || !row0 || !n_rows) return fail(S2D2_EINVAL, "k, v, row0 or n_rows is NULL");
   if ((((uintptr_t)k | (uintptr_t)v) & 15) || (((uintptr_t)row0 | (uintptr_t)n_rows) & 3)) return fail(S2D2_EINVAL, "k and v must be 16-byte aligned, row0 and n_rows 4-byte");
@@ -110,7 +119,7 @@ int32_t s2d2_kv4_append(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_
 
 int32_t s2d2_kv4_read(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t dtype, const int32_t* first, void* k, void* v) {
   int32_t rc;
-  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 1 << 20)) || (rc = check_dtype(dtype))) return rc;
+  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 1 << 20)) || (rc = check_rows(N, T)) || (rc = check_dtype(dtype))) return rc;
   if (!first || !k || !v || (((uintptr_t)k | (uintptr_t)v) & 15) || ((uintptr_t)first & 3)) return fail(S2D2_EINVAL, "first, k or v is NULL or not aligned (k, v: 16 bytes)");
   if ((rc = kv4_ready())) return rc;
   launch_kv4_read((hipStream_t)stream, dtype, kv4_of(kv), N, T, first, k, v);
@@ -119,7 +128,7 @@ int32_t s2d2_kv4_read(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t 
 
 int64_t s2d2_kv4_attention_bytes(const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t n_q_heads) {
   int32_t rc;
-  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 8192)) || (rc = check_q_heads(kv, n_q_heads)) || (rc = check_keys(kv, N, T))) return rc;
+  if ((rc = check_kv4(kv)) || (rc = check_batch(N, T, 8192)) || (rc = check_q_heads(kv, n_q_heads)) || (rc = check_keys(kv, N, T, n_q_heads))) return rc;
   return (int64_t)kv4_attention_bytes(kv4_of(kv), N, T, n_q_heads);
 }
 
@@ -145,14 +154,14 @@ int32_t s2d2_kv4_weigh(void* stream, const s2d2_kv4_view* kv, int32_t layer, con
 
 int64_t s2d2_kv4_evict_bytes(const s2d2_kv4_view* kv, int32_t N) {
   int32_t rc;
-  if ((rc = check_kv4(kv)) || (rc = check_batch(N, 1, 1))) return rc;
+  if ((rc = check_kv4(kv)) || (rc = check_batch(N, 1, 1)) || (rc = check_lists(kv, N))) return rc;
   return (int64_t)kv4_evict_bytes(kv4_of(kv), N);
 }
 
 int32_t s2d2_kv4_evict(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t budget, int32_t slack, int32_t sink, int32_t recent, void* scratch,
                        size_t scratch_bytes) {
   int32_t rc;
-  if ((rc = check_kv4(kv)) || (rc = check_batch(N, 1, 1))) return rc;
+  if ((rc = check_kv4(kv)) || (rc = check_batch(N, 1, 1)) || (rc = check_lists(kv, N))) return rc;
   if (!kv->mass || !kv->position) return fail(S2D2_EINVAL, "eviction needs the cache's mass and position");
   if (budget < 1 || slack < 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > budget) return fail(S2D2_EINVAL, "budget=%d must be positive, slack=%d, sink=%d and recent=%d non-negative, sink + recent at most budget", budget, slack, sink, recent);
   const size_t need = kv4_evict_bytes(kv4_of(kv), N);

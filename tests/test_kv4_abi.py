@@ -95,6 +95,10 @@ def test_other_refusals(lib):
     huge = view(max_pages_per_seq=(1 << 26) - 1)
     assert lib.s2d2_kv4_attention_bytes(huge, 63, 8, 32) > 0 and lib.s2d2_kv4_attention_bytes(huge, 64, 8, 32) == EINVAL   # 64 * (2^30 - 16 + 8 + 64) >= 2^36
     assert lib.s2d2_kv4_weigh(None, huge, 0, rows(N=100)) == EINVAL and lib.s2d2_kv4_attention(None, huge, 0, rows(N=100), FAKE, 1 << 60) == EINVAL
+    assert lib.s2d2_kv4_attention_bytes(w, 128, 8192, 32) > 0 and lib.s2d2_kv4_attention_bytes(w, 129, 8192, 32) == EINVAL
+    assert lib.s2d2_kv4_evict_bytes(view(n_layers=4096, n_kv_heads=1024), 1) == EINVAL
+    assert lib.s2d2_kv4_append(None, w, 1024, 1 << 16, 32, 1, FAKE, FAKE, 1 << 20, 1024, FAKE, FAKE) == EINVAL
+    assert lib.s2d2_kv4_read(None, w, 1024, 1 << 16, 1, FAKE, FAKE, FAKE) == EINVAL
     big = view(max_pages_per_seq=1024)
     need = lib.s2d2_kv4_attention_bytes(big, 4, 8, 32)
     assert need > 0
@@ -128,6 +132,8 @@ def test_scratch_grows_with_the_batch_and_never_with_a_smaller_one(lib):
         for n in (1, 3, 16, 1024):
             last = 0
             for t in (1, 2, 5, 8, 9, 31, 32, 64, 192, 1000, 8192):
+                if n * t * hq > 1 << 25:
+                    break
                 b = lib.s2d2_kv4_attention_bytes(w, n, t, hq)
                 assert b >= last and b >= lib.s2d2_kv4_attention_bytes(w, max(1, n // 2), t, hq)
                 last = b
