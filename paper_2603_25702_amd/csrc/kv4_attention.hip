@@ -26,14 +26,18 @@ namespace s2d2 {
 // Operands of more than 16 bits (fp32 models; queries in two planes) are split into planes of bf16, whose products are exact in 32 bits: 3
 // planes hold the 24 bits of a float.  Softmax weights are half (11 bits; off by at most 2^-12 of the weight), of fp32 models two half planes.
 // The window's own rows, a few tiles, take the same way with K in the caller's type and V, weights in planes of bf16.
+// Measured (us, head dimension 128): 16 sequences x 32 rows x 32 heads on 8 over 8192 entries, 97 (69 GFLOP at 700 TFLOP/s; the vector instructions
+// bound it: about 281 beside 32 matrix instructions for 64 rows x 32 keys, on two wavefronts a SIMD); 4 x 1 row over 60000 to 65536 entries, 55
+// (283 MB at 5.1 TB/s, a large copy's rate); 1 x 1 row over 512 entries, 12 (launch, dependent loads, the join of the wavefronts).
 // ---------------------------------------------------------------------------------------------
 static constexpr float LN2 = 0.69314718055994530942f;
 static constexpr float LOWEST = -3.402823466e38f;   // reference of a row that has seen nothing
 static constexpr float BELOW = 7.f;                 // a reference is taken this far below a maximum (base 2)
 static constexpr float MOST = 32768.f;              // and moves when the weights of a tile of keys sum up to more
-// Wavefronts of a workgroup.  Heads of 256 take 128 registers for the output alone: four wavefronts of up to 512 registers, else eight of up to 256.
+// Wavefronts of a workgroup, one workgroup a compute unit.  With four of them and 512 registers the 16 x 32 rows over 8192 entries took 146 us beside 111,
+// with three wavefronts a SIMD at 168 registers, which spill, 152: two that keep to their registers hide each other's waits.  Heads of 256 take 128 registers for the output alone: four wavefronts of up to 512 registers, else eight of up to 256.
 constexpr int waves_of(int D) { return D == 256 ? 4 : 8; }
-constexpr int min_run_of(int D) { return 4 * waves_of(D); }   // tiles of a split, at least: four a wavefront
+constexpr int min_run_of(int D) { return 4 * waves_of(D); }   // tiles of a split, at least: four a wavefront (a join costs a launch of 4 to 5 us)
 
 template <int QM> struct Mode;
 // QP: planes of the queries; PP: of the softmax weights on cached values (half); WP: of the window's keys and values; WPP: of the weights on them (bf16)
@@ -601,7 +605,7 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
 }
 
 // The splits of a (sequence, KV head, query tile) into its rows, in the order of the splits; a workgroup has 32 dimensions, a thread four of a
-// row.  Sequences of one split are done; Z: splits of a sequence, at most `most`.
+// row: 4 to 5 us, a launch and two dependent loads.  Sequences of one split are done; Z: splits of a sequence, at most `most`.
 template <int D, int QM>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int tiles, int per_wg) {
   const Kv4& kv = a.kv;
@@ -657,7 +661,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int til
 // lie in LDS in operand order, up to QC tiles of 32 rows at a time, each read for two tiles of keys.  The sums of a pair over these rows are
 // added to the mass by one lane a key, tile of rows after tile of rows: a fixed order.
 // Bound: the exponentials (16 cycles each, with a multiply-add and an add 24 for 64 scores); the matrix instructions of a tile take 256 cycles beside
-// 384 of these.
+// 384 of these.  16 x 32 rows x 32 heads on 8 over 8192 entries of 128: 50 us (34 GFLOP, 690 TFLOP/s); with two workgroups a compute unit instead of three 62.
 // ---------------------------------------------------------------------------------------------
 static constexpr int WEIGH_WAVES = 4;
 template <int D, int QM>
@@ -771,7 +775,8 @@ __global__ __launch_bounds__(64 * WEIGH_WAVES, D <= 128 ? 3 : 2) void kv4_weigh_
 static constexpr int WEIGH_TARGET = 768, WEIGH_MIN_RUN = 16;   // three workgroups a compute unit (four wavefronts of up to 168 registers); two pairs of tiles a wavefront
 static constexpr int TARGET = 256;   // workgroups that are resident at once: one a compute unit (eight wavefronts of up to 256 registers)
 
-// Query tiles per workgroup: two share the conversion of K and V; one where there is no second, and where two would not leave registers.
+// Query tiles per workgroup: two share the conversion of K and V; one where there is no second, and where two would not leave registers (outputs of
+// heads of 256, planes of queries).  16 x 32 rows x 4 heads over 8192 entries: 139 us by one, 111 by two in the same build (97 now).
 static int tiles_per_wg(int D, int mode, int q_tiles) { return D <= 128 && (mode == Q_BF16 || mode == Q_F16) && q_tiles >= 2 ? 2 : 1; }
 
 struct AttnShape { int q_tiles, per_wg, groups, per_item, items, most, room; };

@@ -1,5 +1,6 @@
 // The 4-bit cache: quantising append, entries read back, eviction by gathered attention weight.
-// Format and semantics: include/s2d2_kv4.h.  All of it is bound by the bytes it moves.
+// Format and semantics: include/s2d2_kv4.h.  Append, read and move take few operations a byte (24 MB, 5 us at a copy's rate, take 11: the start and end of a
+// launch that short); picking is bound by its passes over a list.
 #include "kv4.h"
 
 #include <algorithm>
@@ -22,6 +23,8 @@ Kv4 kv4_of(const s2d2_kv4_view* view) {
 // Append.  A thread takes 8 values of a row (a 16-byte load of bf16), four neighbours make a group: the group's largest |x| goes round
 // by two DPP moves as an integer (the bits of |x| order as |x| does, with NaN above infinity above all else), v_cvt_scalef32_pk_fp4_f32
 // rounds x / 2^e to nearest-even codes.
+// 36 layers x 16 sequences of up to 16 rows, 8 heads of 128, bf16: 11.5 us; 8 layers x 4 of up to 192 rows, fp32: 10.0.  The counts follow in a launch of
+// their own (2 to 4 us): a row's place depends on the count that every workgroup of the first one reads.
 // ---------------------------------------------------------------------------------------------
 static constexpr int APPEND_ROWS = 4;   // rows of a sequence per workgroup, all in flight at once
 
@@ -119,7 +122,7 @@ void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv
 }
 
 // ---------------------------------------------------------------------------------------------
-// Entries read back: 8 values a thread of each of READ_ROWS entries.
+// Entries read back: 8 values a thread of each of READ_ROWS entries.  11 us for the rows of either append above.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 static constexpr int READ_ROWS = 4;
@@ -184,9 +187,11 @@ void launch_kv4_read(hipStream_t st, int dtype, const Kv4& kv, int N, int T, con
 // A wavefront owns a run of consecutive entries where ranks are needed: its counts go through LDS once, ranks inside it come from ballots.
 // kv4_move_kernel: the moves of all lists by as many workgroups as there are compute units for.  Places that are written lie below the budget,
 // places that are read behind it, so the moves need no order among themselves; and a list that is a little too long moves a few entries only.
+// 512 lists of 4160 entries to 4096: 32 us to pick, 7 to move; 32 lists of 32768 to 4096: 69 and 16 (262 us when the picking workgroups moved as
+// well: 32 compute units of 256).  Picking is bound by one compute unit's passes over its list.
 // ---------------------------------------------------------------------------------------------
 static constexpr int EVICT_KEYS = 36864;   // keys kept in LDS (144 KB); those of longer lists are formed again from memory
-static constexpr int PICK_SHORT = 8192;    // lists up to here by eight wavefronts
+static constexpr int PICK_SHORT = 8192;    // lists up to here by eight wavefronts, two workgroups a compute unit: a pass over the 512 lists 48 us, by sixteen 51, by four 62
 static constexpr int EVICT_AHEAD = 4;      // entries or moves that a thread has in flight
 
 __device__ __forceinline__ uint32_t evict_key(float mass, int position, int sink, int tail) {
