@@ -76,7 +76,8 @@ typedef struct {
 
 /* Rows n_rows[n] (values outside [0, T] are cut) of k, v [n_layers, rows, n_kv_heads, head_dim] in `dtype` from row row0[n] on, layer_stride and
  * row_stride elements apart (16-byte aligned, strides whole 16 bytes), become entries of all layers behind those of sequence n;
- * entries[n] and seq_len[n] advance.  mass of a new entry: 0; position: seq_len[n] + i.  Without room for all of them nothing of that
+ * entries[n] and seq_len[n] advance.  mass of a new entry: 0 (what the rows of its own window gave it is not known here; an eviction right behind
+ * an append should protect its rows, by `recent`); position: seq_len[n] + i.  Without room for all of them nothing of that
  * sequence is written and status[n] is set to S2D2_ENOSPC.  A sequence whose rows leave [0, rows) is skipped.  N <= 1024, N * T below 2^26. */
 int32_t s2d2_kv4_append(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_t T, int32_t rows, int32_t dtype, const void* k, const void* v,
                         int64_t layer_stride, int64_t row_stride, const int32_t* row0, const int32_t* n_rows);
@@ -95,7 +96,7 @@ int32_t s2d2_kv4_attention(void* stream, const s2d2_kv4_view* kv, int32_t layer,
 
 /* mass of every cached entry of `layer` and KV head += sum over the rows of its sequence's window and the query heads of the KV head of
  * exp(scale * q.k - lse): with the lse that s2d2_kv4_attention wrote, the softmax weights that the rows gave the entry.  A row of lse -inf adds
- * nothing.  k, v, lo, hi and out are not looked at (out may be NULL).  N <= 1024, T <= 8192. */
+ * nothing.  The window's own rows, which are no entries yet, get nothing (a single token can be appended first, and then attend to the entries alone).  k, v, lo, hi and out are not looked at (out may be NULL).  N <= 1024, T <= 8192. */
 int32_t s2d2_kv4_weigh(void* stream, const s2d2_kv4_view* kv, int32_t layer, const s2d2_kv4_rows* rows);
 
 /* Every sequence with more than budget + slack entries is cut to `budget`, list by list (a list: one layer, one KV head).  Kept are the entries of the
@@ -115,7 +116,8 @@ int64_t s2d2_kv4_evict_bytes(const s2d2_kv4_view* kv, int32_t N);
  * Their views then have to describe it: k_pages = k_codes, v_pages = v_codes, the same page_table, seq_len, n_pages, page_size and
  * max_pages_per_seq (else S2D2_EINVAL).  n_layers, n_kv_heads and head_dim must be the model's.  Rows of a window are attended to at the model's
  * precision and quantised when they are appended.  With mass, s2d2_verify, s2d2_prefill and s2d2_block_complete add the weights of their windows' rows
- * (the drafting forward adds none), and s2d2_kv4_evict on the same cache may follow an append at any time: positions go by seq_len.
+ * (the drafting forward adds none), to the cached entries and to the rows that they see among themselves: the context's next append enters its rows with the mass
+ * that the last of these forwards gave them (0 if there was none since this call).  s2d2_kv4_evict on the same cache may follow an append at any time: positions go by seq_len.
  * lse: device [s2d2_stage_rows(max_batch, max_block), n_q_heads] fp32, needed with mass; scratch: device, 16-byte aligned, at least
  * s2d2_kv4_attention_bytes(kv, max_batch, 3 * max_block, n_q_heads) bytes.  Both belong to the context while it runs. */
 int32_t s2d2_set_kv4(s2d2_ctx* ctx, const s2d2_kv4_view* kv, void* scratch, size_t scratch_bytes, float* lse);

@@ -92,6 +92,7 @@ struct s2d2_ctx {
   Kv4 kv4;
   void* kv4_scratch;
   float* kv4_lse;           // [rows_cap, Hq], with kv4.mass
+  float* kv4_row_mass;      // [n_layers, rows_cap, Hkv] what the rows of the last staged forward gave each other; goes with them into the cache
   // profiling (measurement aid)
   bool prof_on;
   int32_t prof_cap;
@@ -237,6 +238,7 @@ size_t carve(s2d2_ctx* c, uint8_t* base) {
   c->vws.sample_tiles = cv.take<float>(tile_sum_floats(sample_rows_shared((int)LR), d.vocab));
   c->vws.sample_arrive = cv.take<int32_t>((size_t)sample_rows_shared((int)LR) * ARRIVE_STRIDE);
   c->vws.arrive = cv.take<int32_t>(LR * ARRIVE_STRIDE);
+  c->kv4_row_mass = cv.take<float>((size_t)d.n_layers * R * d.n_kv_heads);
   return (cv.off + 255) & ~(size_t)255;
 }
 
@@ -468,6 +470,7 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
       x.out = c->obuf; x.o_ld = ld_o; x.o_lo = lo_o; x.lse = weigh ? c->kv4_lse : nullptr;
       x.scale_log2e = 1.44269504088896340736f / sqrtf((float)d.head_dim);
       { ProfScope ps(c, 1, 0.0); launch_kv4_attention(st, mode4, x, l, c->kv4_scratch); }
+      x.row_mass = weigh ? c->kv4_row_mass + (size_t)l * c->rows_cap * d.n_kv_heads : nullptr;
       if (weigh) { ProfScope ps(c, 1, 0.0); launch_kv4_weigh(st, mode4, x, l); }
       if (LR == 0 && l == d.n_layers - 1) return check_launch("forward");
     } else if (wide) {
@@ -744,7 +747,9 @@ int32_t s2d2_set_kv4(s2d2_ctx* c, const s2d2_kv4_view* kv, void* scratch, size_t
   c->kv4_scratch = scratch;
   c->kv4_lse = lse;
   c->kv4_on = true;
-  return S2D2_OK;
+  if (kv->mass)   // (an append that no forward went ahead of)
+    for (int l = 0; l < d.n_layers; ++l) launch_fill_i32(c->stream, (int32_t*)c->kv4_row_mass + (size_t)l * c->rows_cap * d.n_kv_heads, c->rows_cap * d.n_kv_heads, 0);
+  return check_launch("s2d2_set_kv4");
 }
 
 static int32_t check_params(const s2d2_params* p) {
@@ -854,7 +859,8 @@ static void append_staged(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, int32_
   const s2d2_model_desc& d = c->desc;
   if (c->kv4_on) {
     const int64_t width = (int64_t)d.n_kv_heads * d.head_dim;
-    launch_kv4_append(c->stream, d.dtype, c->kv4, N, Kv4Rows{row0, lead, n_accept, span_len, hold_back, most, c->rows_cap}, k_stage, v_stage, c->rows_cap * width, width);
+    launch_kv4_append(c->stream, d.dtype, c->kv4, N, Kv4Rows{row0, lead, n_accept, span_len, hold_back, most, c->rows_cap}, k_stage, v_stage, c->rows_cap * width, width,
+                      c->kv4.mass ? c->kv4_row_mass : nullptr, (int64_t)c->rows_cap * d.n_kv_heads);
     return;
   }
   launch_kv_append(c->stream, d.dtype, d.n_layers, N, c->rows_cap, geom(c, kv), kv->k_pages, kv->v_pages, k_stage, v_stage, row0, lead, span_len, n_accept,

@@ -54,6 +54,8 @@ struct Kv4Attn {
   const int32_t *row0, *n_rows, *lo, *hi;
   void* out;
   float* lse;
+  float* row_mass;     // weighing: [rows, KV heads], what the window's rows give each other (k, lo and hi needed), or NULL
+  const void* window_k;   // weighing: the window's keys
   float scale_log2e;   // scores to base 2
   float *part_o, *part_ml;
   int2* part_of;     // [N] of a sequence with several splits: its first item, its splits
@@ -64,6 +66,7 @@ struct Kv4Attn {
   int32_t room;      // splits beyond one a sequence that the scratch holds
   int32_t target;    // workgroups to aim for
   int32_t min_run;   // tiles of a split, at least
+  int32_t cached_wgs;  // weighing: workgroups of the cached entries; those of the window's tiles follow
   Divisor group;     // by query heads per KV head
 };
 
@@ -84,7 +87,9 @@ struct Kv4Rows {
     return row0[n] < 0 || c < 0 ? 0 : min(c, most);
   }
 };
-void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv4Rows& r, const void* k, const void* v, int64_t layer_stride, int64_t row_stride);
+// row_mass: [layers, mass_stride / KV heads rows, KV heads], the mass that the rows bring along; NULL: 0
+void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv4Rows& r, const void* k, const void* v, int64_t layer_stride, int64_t row_stride,
+                       const float* row_mass, int64_t mass_stride);
 void launch_kv4_read(hipStream_t st, int dtype, const Kv4& kv, int N, int T, const int32_t* first, void* k, void* v);
 void launch_kv4_evict(hipStream_t st, const Kv4& kv, int N, int budget, int slack, int sink, int recent, void* scratch);
 size_t kv4_evict_bytes(const Kv4& kv, int N);

@@ -113,7 +113,7 @@ int32_t s2d2_kv4_append(void* stream, const s2d2_kv4_view* kv, int32_t N, int32_
   if (!stride_ok(row_stride, width, dtype)) return fail(S2D2_EINVAL, "row_stride must be whole 16 bytes and at least %lld elements", (long long)width);
   if (layer_stride < 0 || layer_stride % e || layer_stride >= (1ll << 50) || (kv->n_layers > 1 && layer_stride < width)) return fail(S2D2_EINVAL, "layer_stride must be whole 16 bytes and at least a row");
   if ((rc = kv4_ready())) return rc;
-  launch_kv4_append((hipStream_t)stream, dtype, kv4_of(kv), N, Kv4Rows{row0, n_rows, nullptr, nullptr, 0, T, rows}, k, v, layer_stride, row_stride);
+  launch_kv4_append((hipStream_t)stream, dtype, kv4_of(kv), N, Kv4Rows{row0, n_rows, nullptr, nullptr, 0, T, rows}, k, v, layer_stride, row_stride, nullptr, 0);
   return check_launch("s2d2_kv4_append");
 }
 

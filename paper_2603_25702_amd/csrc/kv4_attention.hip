@@ -669,11 +669,78 @@ static constexpr int QC = D * Mode<QM>::QP <= 384 ? 4 : 2;
 template <int D, int QM>
 static constexpr size_t weigh_lds() { return (size_t)QC<D, QM> * (32 * D * 2 * Mode<QM>::QP + 33 * sizeof(float)); }
 
+// The weights that a window's rows give each other, into row_mass: a workgroup has one sequence, one KV head and 32 keys, a wavefront every fourth tile of
+// 32 query rows that sees one of them (of a causal window half the tiles).  S = Q K^T as below, keys and queries from memory; the wavefronts' sums are added up
+// in their order.  Verification windows of 16 x 32 rows have 128 of these workgroups beside the 768 of their cached entries, in one launch.
 template <int D, int QM>
+__device__ __forceinline__ void weigh_window(const Kv4Attn& a, int block, uint8_t* s_mem) {
+  typedef typename Mode<QM>::T T;
+  constexpr int QP = Mode<QM>::QP, WP = Mode<QM>::WP, NW = WEIGH_WAVES, DS = D / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+  const int kvh = block % a.kv.H, tiles = (a.T + 31) >> 5, key0 = block / a.kv.H % tiles * 32;
+  const SeqTiles sq = seq_tiles(a, block / a.kv.H / tiles);
+  if (key0 >= sq.rows) return;
+  float* s_ref = (float*)s_mem + wave * 32;                              // [NW][32] minus a row's lse to base 2; -inf: the row adds nothing
+  int4* s_row = (int4*)(s_mem + NW * 32 * sizeof(float)) + wave * 32;    // [NW][32] the row and the rows that it sees
+  float* s_sum = (float*)(s_mem + NW * 32 * (sizeof(float) + sizeof(int4)));   // [NW][32]
+  const int key = sq.row0 + min(key0 + c, sq.rows - 1), k0 = sq.row0 + key0, k1 = sq.row0 + min(key0 + 32, sq.rows), nq = sq.rows * a.grp;
+  float sum = 0.f;
+  for (int q0 = wave * 32; q0 < nq; q0 += NW * 32) {
+    const int qi = min(q0 + c, nq - 1), r = a.group.div(qi), row = sq.row0 + r, head = kvh * a.grp + qi - r * a.grp;
+    const int lo = a.lo[row], hi = a.hi[row];
+    if (!__ballot((lo < k1 && hi > k0) || (row >= k0 && row < k1))) continue;
+    const float lse = a.lse[(size_t)row * a.Hq + head];
+    if (h == 0) {
+      s_ref[c] = q0 + c >= nq || lse == -INFINITY ? -INFINITY : -lse * (1.f / LN2);
+      s_row[c] = make_int4(row, lo, hi, 0);
+    }
+    f32x16_t s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) {
+      u32x4_t q[QP], k[WP];
+      load_planes<QP>((const T*)a.q + row * a.q_ld + (size_t)head * D + h * (D / 2) + 8 * ds, a.q_lo, q);
+      load_planes<WP>((const T*)a.window_k + key * a.kv_ld + (size_t)kvh * D + h * (D / 2) + 8 * ds, 0, k);
+#pragma unroll
+      for (int e = 0; e < WP; ++e)
+#pragma unroll
+        for (int p = 0; p < QP; ++p)
+          if (e + p < (QP > WP ? QP : WP)) s = score_mfma<QM>(q[p], k[e], s);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int rr = 8 * (i >> 2) + 4 * h + (i & 3);
+      const float ref = s_ref[rr];
+      const int4 see = s_row[rr];
+      const bool seen = (key >= see.y && key < see.z) || key == see.x;
+      sum += seen && ref != -INFINITY ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2e, ref)) : 0.f;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  sum += __shfl_xor(sum, 32, 64);
+  if (h == 0) s_sum[wave * 32 + c] = sum;
+  __syncthreads();
+  if (wave == 0 && h == 0 && key0 + c < sq.rows) {
+#pragma unroll
+    for (int w = 1; w < NW; ++w) sum += s_sum[w * 32 + c];
+    a.row_mass[(size_t)key * a.kv.H + kvh] = sum;
+  }
+}
+
+// WINDOW: the window's own rows too, by the workgroups from cached_wgs on
+template <int D, int QM, bool WINDOW>
 __global__ __launch_bounds__(64 * WEIGH_WAVES, D <= 128 ? 3 : 2) void kv4_weigh_kernel(const Kv4Attn a, int layer) {
   typedef typename Mode<QM>::T T;
   constexpr int QP = Mode<QM>::QP, NW = WEIGH_WAVES, DS = D / 16, C = QC<D, QM>;
   extern __shared__ __attribute__((aligned(16))) uint8_t s_mem[];
+  if (WINDOW && (int)blockIdx.x >= a.cached_wgs) {
+    weigh_window<D, QM>(a, blockIdx.x - a.cached_wgs, s_mem);
+    return;
+  }
   u32x4_t* s_q = (u32x4_t*)s_mem;                       // [C][DS][QP][64]
   float* s_ref = (float*)(s_q + C * DS * QP * 64);      // [C][32] minus a row's lse to base 2; -inf: the row adds nothing
   int* s_some = (int*)(s_ref + C * 32);                 // [C] whether there is such a row
@@ -849,20 +916,29 @@ void launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void*
 }
 
 void launch_kv4_weigh(hipStream_t st, int mode, Kv4Attn& a, int layer) {
-  a.k = a.v = nullptr;
+  a.window_k = a.row_mass ? a.k : nullptr;
+  a.k = a.v = nullptr;   // (the runs are those of the cached entries)
   a.per_item = a.kv.H;
   a.room = 1 << 30;
   a.target = WEIGH_TARGET;
   a.min_run = WEIGH_MIN_RUN;
   const int most = std::max(1, ((a.kv.cap + 31) / 32 + WEIGH_MIN_RUN - 1) / WEIGH_MIN_RUN);
   a.items = (int)std::min<long long>((long long)a.N * most, (WEIGH_TARGET + a.kv.H - 1) / a.kv.H + (long long)a.N);
+  a.cached_wgs = a.items * a.kv.H;
   by_head_dim(a.kv.D, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    const dim3 grid(a.items * a.kv.H), wg(64 * WEIGH_WAVES);
-    if (mode == Q_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32>), grid, wg, (weigh_lds<D, Q_F32>()), st, a, layer);
-    else if (mode == Q_BF16X2) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16X2>), grid, wg, (weigh_lds<D, Q_BF16X2>()), st, a, layer);
-    else if (mode == Q_F16) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F16>), grid, wg, (weigh_lds<D, Q_F16>()), st, a, layer);
-    else S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16>), grid, wg, (weigh_lds<D, Q_BF16>()), st, a, layer);
+    const dim3 wg(64 * WEIGH_WAVES);
+    if (a.row_mass) {   // (forwards)
+      const dim3 grid(a.cached_wgs + a.N * a.kv.H * ((a.T + 31) / 32));
+      if (mode == Q_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32, true>), grid, wg, (weigh_lds<D, Q_F32>()), st, a, layer);
+      else if (mode == Q_BF16X2) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16X2, true>), grid, wg, (weigh_lds<D, Q_BF16X2>()), st, a, layer);
+      else if (mode == Q_F16) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F16, true>), grid, wg, (weigh_lds<D, Q_F16>()), st, a, layer);
+      else S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16, true>), grid, wg, (weigh_lds<D, Q_BF16>()), st, a, layer);
+    } else {
+      const dim3 grid(a.cached_wgs);
+      if (mode == Q_F32) S2D2_LAUNCH((kv4_weigh_kernel<D, Q_F32, false>), grid, wg, (weigh_lds<D, Q_F32>()), st, a, layer);
+      else S2D2_LAUNCH((kv4_weigh_kernel<D, Q_BF16, false>), grid, wg, (weigh_lds<D, Q_BF16>()), st, a, layer);
+    }
   });
 }
 
@@ -877,10 +953,12 @@ int kv4_attention_init() {
       limit((const void*)kv4_attention_kernel<D, Q_BF16X2, 1>, attn_lds<D, 1>());
       limit((const void*)kv4_attention_kernel<D, Q_F32, 1>, attn_lds<D, 1>());
       limit((const void*)kv4_attention_kernel<D, Q_F16, 1>, attn_lds<D, 1>());
-      limit((const void*)kv4_weigh_kernel<D, Q_F16>, weigh_lds<D, Q_F16>());
-      limit((const void*)kv4_weigh_kernel<D, Q_BF16>, weigh_lds<D, Q_BF16>());
-      limit((const void*)kv4_weigh_kernel<D, Q_BF16X2>, weigh_lds<D, Q_BF16X2>());
-      limit((const void*)kv4_weigh_kernel<D, Q_F32>, weigh_lds<D, Q_F32>());
+      limit((const void*)kv4_weigh_kernel<D, Q_BF16, false>, weigh_lds<D, Q_BF16>());
+      limit((const void*)kv4_weigh_kernel<D, Q_F32, false>, weigh_lds<D, Q_F32>());
+      limit((const void*)kv4_weigh_kernel<D, Q_BF16, true>, weigh_lds<D, Q_BF16>());
+      limit((const void*)kv4_weigh_kernel<D, Q_BF16X2, true>, weigh_lds<D, Q_BF16X2>());
+      limit((const void*)kv4_weigh_kernel<D, Q_F16, true>, weigh_lds<D, Q_F16>());
+      limit((const void*)kv4_weigh_kernel<D, Q_F32, true>, weigh_lds<D, Q_F32>());
       constexpr int D2 = D <= 128 ? D : 128;
       limit((const void*)kv4_attention_kernel<D2, Q_BF16, 2>, attn_lds<D2, 2>());
       limit((const void*)kv4_attention_kernel<D2, Q_F16, 2>, attn_lds<D2, 2>());

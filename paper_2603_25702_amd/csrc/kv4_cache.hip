@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t kv4_quantise(const float (&x)[8], uint32_t& 
 
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4 kv, Kv4Rows r, int per_seq, const T* __restrict__ k, const T* __restrict__ v,
-                                                         int64_t layer_stride, int64_t row_stride) {
+                                                         int64_t layer_stride, int64_t row_stride, const float* __restrict__ row_mass, int64_t mass_stride) {
   const int n = blockIdx.x / per_seq, l = blockIdx.y;
   const int rows = r.count(n), S = kv.held(n), t0 = (blockIdx.x % per_seq) * APPEND_ROWS;
   if (t0 >= rows || r.row0[n] > r.rows - rows || S + rows > kv.cap) return;   // (the commit flags a sequence without room)
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4 kv, Kv4Rows r, int 
       ((uint32_t*)((value ? kv.vc : kv.kc) + at * (kv.D / 2)))[part] = codes;
       if ((part & 3) == 0) (value ? kv.vs : kv.ks)[at * (kv.D / 32) + part / 4] = (uint8_t)scale;
       if (part == 0 && !value) {
-        if (kv.mass) kv.mass[at] = 0.f;
+        if (kv.mass) kv.mass[at] = row_mass ? row_mass[l * mass_stride + (int64_t)(r.row0[n] + t0 + t) * kv.H + head] : 0.f;
         if (kv.position) kv.position[at] = pos0 + t0 + t;
       }
     }
@@ -111,13 +111,14 @@ __global__ void kv4_append_commit_kernel(Kv4 kv, Kv4Rows r, int N) {
   kv.seq_len[n] += rows;
 }
 
-void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv4Rows& r, const void* k, const void* v, int64_t layer_stride, int64_t row_stride) {
+void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv4Rows& r, const void* k, const void* v, int64_t layer_stride, int64_t row_stride,
+                       const float* row_mass, int64_t mass_stride) {
   const int per_seq = (r.most + APPEND_ROWS - 1) / APPEND_ROWS;
   const dim3 grid(N * per_seq, kv.n_layers);
   if (dtype == S2D2_BF16)
-    S2D2_LAUNCH(kv4_append_kernel<bf16_t>, grid, dim3(256), 0, st, kv, r, per_seq, (const bf16_t*)k, (const bf16_t*)v, layer_stride, row_stride);
+    S2D2_LAUNCH(kv4_append_kernel<bf16_t>, grid, dim3(256), 0, st, kv, r, per_seq, (const bf16_t*)k, (const bf16_t*)v, layer_stride, row_stride, row_mass, mass_stride);
   else
-    S2D2_LAUNCH(kv4_append_kernel<float>, grid, dim3(256), 0, st, kv, r, per_seq, (const float*)k, (const float*)v, layer_stride, row_stride);
+    S2D2_LAUNCH(kv4_append_kernel<float>, grid, dim3(256), 0, st, kv, r, per_seq, (const float*)k, (const float*)v, layer_stride, row_stride, row_mass, mass_stride);
   S2D2_LAUNCH(kv4_append_commit_kernel, dim3((N + 255) / 256), dim3(256), 0, st, kv, r, N);
 }
 
