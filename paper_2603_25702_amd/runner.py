@@ -21,14 +21,18 @@ class Session:
     """cache_bits = 4 keeps the prefix in a 4-bit cache (include/s2d2_kv4.h).  With a budget that cache is bounded: after every append, and
     between the chunks of a prompt, a sequence with more than budget + slack entries keeps `budget` of them in every layer and KV head, the first
     `sink` and the last `recent` positions and those that gathered the most attention weight; max_seq then is the room for
-    budget + slack entries and the rows of one append."""
+    budget + slack entries and the rows of one append.  `recent` is half of what the sink leaves of the budget, and at least the 2 * B rows of an append if they
+    fit: weight accumulates, so that new entries lose against old ones as long as few rows have seen them."""
 
     def __init__(self, cfg, weights: Dict[str, torch.Tensor], N: int, B: int, max_seq: int, page_size: int = 16,
                  device: str = "cuda:0", page_table: Optional[np.ndarray] = None, max_block: Optional[int] = None,
                  act_planes: int = 0, cache_bits: int = 16, budget: Optional[int] = None, slack: int = 0, sink: int = 4,
-                 recent: int = 0):
+                 recent: Optional[int] = None):
         if cache_bits not in (4, 16) or (budget is not None and cache_bits != 4):
             raise ValueError("cache_bits is 16 (the model's own type) or 4, and only a 4-bit cache has a budget")
+        if budget is not None and recent is None:
+            left = max(0, budget - sink)
+            recent = max(left // 2, min(2 * B, left))
         if budget is not None and not (budget >= 1 and slack >= 0 and sink >= 0 and recent >= 0 and sink + recent <= budget):
             raise ValueError("a budget is positive, slack, sink and recent are not negative, and sink + recent fit in the budget")
         self.bound = None if budget is None else (budget, slack, sink, recent)
