@@ -86,6 +86,7 @@ class Session:
         self.kv.seq_len.zero_()
         if self.four:
             self.kv.entries.zero_()
+            self.kv.status.zero_()   # (what an earlier prompt or block lacked)
         if longest:
             chunks = (longest + most - 1) // most
             T = (longest + chunks - 1) // chunks
@@ -99,7 +100,7 @@ class Session:
                 self._evict()
         torch.cuda.synchronize(self.dev)
         if self.four and int(self.kv.status.abs().sum()):
-            raise RuntimeError(f"prefill: device status {self.kv.status.cpu().tolist()}: the cache has no room for a chunk of {T} tokens")
+            raise RuntimeError(f"prefill: device status {self.kv.status.cpu().tolist()}: the cache has no room for prompts of {cached} tokens")
         entries = self.kv.entries.clone() if self.four else None
         self.reset_blocks(lens, last)
         if self.four:

@@ -51,3 +51,37 @@ def test_new_tokens_outlive_their_append_at_the_defaults(cfg, budget):
     assert min(grown) > 15
     for n, prompt in enumerate((391, 120)):
         assert ((positions(kv, n) >= prompt).sum(1) >= min(grown[n], (budget - 4) // 2)).all()
+
+
+# ---- a session that once had no room ----
+
+def test_a_prompt_that_fits_after_one_that_did_not():
+    cfg = TINY
+    ses = Session(cfg, I.gen_weights(cfg, 3), 1, 4, 64, cache_bits=4)
+    good = prompts(cfg, [30])
+    fresh = Session(cfg, I.gen_weights(cfg, 3), 1, 4, 64, cache_bits=4)
+    fresh.prefill(good)
+    for _ in range(2):
+        with pytest.raises(RuntimeError, match="status"):
+            ses.prefill(prompts(cfg, [100]))
+        ses.prefill(good)
+        assert ses.kv.entries.tolist() == [30] == ses.kv.seq_len.tolist() and not ses.kv.status.any()
+        assert ses.generate(Params(seed=3, tau=0.3), RouteParams(), 1, 5) == fresh.generate(Params(seed=3, tau=0.3), RouteParams(), 1, 5)
+        fresh.prefill(good)
+    # a sequence that ran out of room while it was generated
+    with pytest.raises(RuntimeError, match="status"):
+        ses.prefill(prompts(cfg, [60]))
+        ses.generate(Params(seed=3, tau=0.0), RouteParams(), 4, 5)
+    ses.prefill(good)
+    assert ses.kv.entries.tolist() == [30]
+
+
+def test_a_prompt_of_one_token_after_a_lack_of_room():
+    """A right-shifted model caches nothing of it: no chunk, no room needed."""
+    import dataclasses
+    cfg = dataclasses.replace(TINY, right_shifted=True)
+    ses = Session(cfg, I.gen_weights(cfg, 3), 1, 4, 64, cache_bits=4)
+    with pytest.raises(RuntimeError, match="status"):
+        ses.prefill(prompts(cfg, [100]))
+    ses.prefill(prompts(cfg, [1]))
+    assert ses.kv.entries.tolist() == [0] == ses.kv.seq_len.tolist()
