@@ -75,8 +75,9 @@ class Session:
 
     def prefill(self, ids: Sequence[np.ndarray]):
         """Fills the cache with the causal K/V of the prompts: one upload, then one forward per chunk of up to
-        3 * max_block tokens of every sequence (equal chunks), all enqueued without a wait in between."""
-        N, most = self.N, 3 * self.eng.max_block
+        3 * max_block tokens of every sequence (equal chunks; in a bounded cache shorter ones where it has no room for
+        these), all enqueued without a wait in between."""
+        N = self.N
         lens = [len(x) for x in ids]
         last = [int(x[-1]) for x in ids]
         if self.four and getattr(self.cfg, "right_shifted", False):   # (the carried last token gets no entry: there may be no telling which one it is)
@@ -88,8 +89,8 @@ class Session:
             self.kv.entries.zero_()
             self.kv.status.zero_()   # (what an earlier prompt or block lacked)
         if longest:
-            chunks = (longest + most - 1) // most
-            T = (longest + chunks - 1) // chunks
+            T = self._chunk(cached)
+            chunks = (longest + T - 1) // T
             host = np.zeros((N, chunks * T), dtype=np.int32)
             for n in range(N):
                 host[n, :cached[n]] = ids[n]
@@ -105,6 +106,28 @@ class Session:
         self.reset_blocks(lens, last)
         if self.four:
             self.kv.entries.copy_(entries)
+
+    def _chunk(self, cached: Sequence[int]) -> int:
+        """Tokens of a prompt chunk: as few equal chunks as the workspace takes and the cache, cut between them, has room for."""
+        longest, cap, last = max(cached), self.kv.page_table.shape[1] * self.kv.page_size if self.bound else 0, 0
+        for most in range(3 * self.eng.max_block, 0, -1):
+            chunks = (longest + most - 1) // most
+            T = (longest + chunks - 1) // chunks
+            if T != last and (not self.bound or all(self._fits(n, T, cap) for n in cached)):
+                return T
+            last = T
+        return min(longest, 3 * self.eng.max_block)   # (no room, however short: the appends report it)
+
+    def _fits(self, tokens: int, T: int, cap: int) -> bool:
+        budget, slack = self.bound[:2]
+        held = 0
+        for at in range(0, tokens, T):
+            held += min(T, tokens - at)
+            if held > cap:
+                return False
+            if held > budget + slack:
+                held = budget
+        return True
 
     def reset_blocks(self, seq_lens: Sequence[int], last_tokens: Optional[Sequence[int]] = None):
         """Fresh [MASK]^B block right after the prefix of every sequence.  For a right-shifted model the last prefix

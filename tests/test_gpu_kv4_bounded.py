@@ -85,3 +85,31 @@ def test_a_prompt_of_one_token_after_a_lack_of_room():
         ses.prefill(prompts(cfg, [100]))
     ses.prefill(prompts(cfg, [1]))
     assert ses.kv.entries.tolist() == [0] == ses.kv.seq_len.tolist()
+
+
+# ---- room ----
+
+@pytest.mark.parametrize("budget,slack,length", [(100, 8, 391), (40, 0, 200), (16, 0, 193)])
+def test_prompts_of_any_length_in_the_room_that_is_promised(budget, slack, length):
+    """Room for budget + slack entries and the rows of one append: chunks of a prompt are no longer than that."""
+    cfg, B = TINY, 4
+    ses = Session(cfg, I.gen_weights(cfg, 3), 2, B, budget + slack + 2 * B, page_size=4, cache_bits=4, budget=budget, slack=slack)
+    ses.prefill(prompts(cfg, [length, 20]))
+    assert ses.kv.seq_len.tolist() == [length, 20] and ses.kv.entries.tolist()[0] <= budget + slack
+    out, _ = ses.generate(Params(seed=2, tau=0.2), RouteParams(), 3, 5)
+    assert all(len(o) == 12 for o in out)
+
+
+def test_chunks_stay_as_they_are_where_there_is_room():
+    """Chunks of 131 of a prompt of 391 go into 240 places with a budget of 100: the entries in front of a chunk are the budget, not what it may grow to."""
+    cfg = TINY
+    W, ids = I.gen_weights(cfg, 3), prompts(cfg, [391])
+    wide, tight = (Session(cfg, W, 1, 4, room, cache_bits=4, budget=100, slack=16) for room in (640, 240))
+    calls = []
+    for ses in (wide, tight):
+        call, here = ses.eng.s2d2_prefill, []
+        ses.eng.s2d2_prefill = lambda kv, N, T, *a, call=call, here=here: (here.append(T), call(kv, N, T, *a))
+        ses.prefill(ids)
+        calls.append(here)
+    assert calls == [[131, 131, 131]] * 2
+    assert np.array_equal(positions(wide.kv, 0), positions(tight.kv, 0))
