@@ -102,10 +102,7 @@ class Session:
         torch.cuda.synchronize(self.dev)
         if self.four and int(self.kv.status.abs().sum()):
             raise RuntimeError(f"prefill: device status {self.kv.status.cpu().tolist()}: the cache has no room for prompts of {cached} tokens")
-        entries = self.kv.entries.clone() if self.four else None
         self.reset_blocks(lens, last)
-        if self.four:
-            self.kv.entries.copy_(entries)
 
     def _chunk(self, cached: Sequence[int]) -> int:
         """Tokens of a prompt chunk: as few equal chunks as the workspace takes and the cache, cut between them, has room for."""
@@ -132,20 +129,28 @@ class Session:
     def reset_blocks(self, seq_lens: Sequence[int], last_tokens: Optional[Sequence[int]] = None):
         """Fresh [MASK]^B block right after the prefix of every sequence.  For a right-shifted model the last prefix
         token is carried in front of the block instead of being counted as cached (its row scores the block's
-        first position), so `last_tokens` is required there."""
+        first position), so `last_tokens` is required there.  A 4-bit cache goes back to the first entries of its
+        sequences; one that was cut holds other positions in every list and has to stay where it is."""
+        t = torch.as_tensor(list(seq_lens), dtype=torch.int32)
+        pos0, shifted = t, getattr(self.cfg, "right_shifted", False)
+        if shifted:
+            if last_tokens is None:
+                raise ValueError("a right-shifted model needs the last prefix token of every sequence")
+            t = t - 1
+        if self.four:
+            entries, cached = self.kv.entries.cpu(), self.kv.seq_len.cpu()
+            cut = entries != cached
+            if bool((cut & (t != cached)).any()):
+                raise ValueError(f"entries were evicted from sequences {cut.nonzero().flatten().tolist()}: they cannot go from {cached.tolist()} cached tokens to {t.tolist()}")
         self.st = self._state(self.B)
         self.st.block_tokens.fill_(self.cfg.mask_id)
         self.st.carry_tokens.zero_()
-        t = torch.as_tensor(list(seq_lens), dtype=torch.int32)
-        self.st.block_pos0.copy_(t)
-        if getattr(self.cfg, "right_shifted", False):
-            if last_tokens is None:
-                raise ValueError("a right-shifted model needs the last prefix token of every sequence")
+        self.st.block_pos0.copy_(pos0)
+        if shifted:
             self.st.carry_tokens[:, 0].copy_(torch.as_tensor(list(last_tokens), dtype=torch.int32))
-            t = t - 1
         self.kv.seq_len.copy_(t)
         if self.four:
-            self.kv.entries.copy_(t)
+            self.kv.entries.copy_(torch.where(cut, entries, t))
         self.kv.status.zero_()
         self.step_dev.zero_()
 

@@ -113,3 +113,31 @@ def test_chunks_stay_as_they_are_where_there_is_room():
         calls.append(here)
     assert calls == [[131, 131, 131]] * 2
     assert np.array_equal(positions(wide.kv, 0), positions(tight.kv, 0))
+
+
+# ---- fresh blocks ----
+
+def test_fresh_blocks_behind_a_cache_that_was_cut():
+    cfg = SMALL_BF16
+    lens = [200, 30]
+    ses = Session(cfg, I.gen_weights(cfg, 3), 2, 4, 320, cache_bits=4, budget=64)
+    ses.prefill(prompts(cfg, lens))
+    prm, kv = Params(seed=1), ses.kv
+    ses.eng.s2d2_draft(kv, ses.st, 2, 4, prm, ses.d)
+    want = ses.d.logits.clone()
+    ses.reset_blocks(lens)                       # where they are already
+    assert kv.entries.tolist() == [64, 30] and kv.seq_len.tolist() == lens
+    ses.eng.s2d2_draft(kv, ses.st, 2, 4, prm, ses.d)
+    assert torch.equal(ses.d.logits, want)
+    for step in range(4):
+        ses.step(Params(seed=1, step=step, tau=0.0))
+    now, held = kv.seq_len.tolist(), kv.entries.tolist()
+    assert held[0] == 64 and now[0] > 200 and held[1] == now[1] > 30
+    with pytest.raises(ValueError, match="evicted"):
+        ses.reset_blocks(lens)                   # which of the first sequence's entries lie before 200 differs from list to list
+    assert kv.seq_len.tolist() == now and kv.entries.tolist() == held
+    ses.reset_blocks([now[0], 25])               # the second one's are in order: back to 25
+    assert kv.seq_len.tolist() == [now[0], 25] and kv.entries.tolist() == [64, 25]
+    ses.prefill(prompts(cfg, lens))              # and from the start again
+    ses.eng.s2d2_draft(kv, ses.st, 2, 4, prm, ses.d)
+    assert torch.equal(ses.d.logits, want)
