@@ -366,7 +366,7 @@ class Engine:
         if need < 0:
             raise S2D2Error(int(need), self.lib.s2d2_last_error().decode())
         self.workspace = torch.empty(int(need), dtype=torch.uint8, device=self.device)
-        self.stream = stream
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)   # the context keeps it: work that belongs to it goes there
         pbytes = int(self.lib.s2d2_packed_bytes(C.byref(self.desc))) if packed else 0
         self.packed = torch.empty(pbytes, dtype=torch.uint8, device=self.device) if pbytes > 0 else None
         ctx = C.c_void_p()
@@ -377,8 +377,7 @@ class Engine:
         self.stage_rows = int(self.lib.s2d2_stage_rows(max_batch, max_block))
 
     def _stream_handle(self):
-        s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
-        return C.c_void_p(s.cuda_stream)
+        return C.c_void_p(self.stream.cuda_stream)
 
     def set_stream(self, stream: torch.cuda.Stream):
         self.stream = stream

@@ -141,3 +141,30 @@ def test_fresh_blocks_behind_a_cache_that_was_cut():
     ses.prefill(prompts(cfg, lens))              # and from the start again
     ses.eng.s2d2_draft(kv, ses.st, 2, 4, prm, ses.d)
     assert torch.equal(ses.d.logits, want)
+
+
+# ---- streams ----
+
+def test_eviction_runs_on_the_stream_of_the_forwards():
+    """Sessions that are made under one stream and stepped under another."""
+    cfg = SMALL_BF16
+    W, ids, runs = I.gen_weights(cfg, 3), prompts(cfg, [200, 90]), []
+    side = torch.cuda.Stream()
+    for made, stepped in ((None, None), (None, side), (side, None)):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(made):
+            ses = Session(cfg, W, 2, 4, 320, cache_bits=4, budget=64, recent=8)
+            ses.prefill(ids)
+        torch.cuda.synchronize()
+        seen = []
+        with torch.cuda.stream(stepped):
+            for step in range(6):
+                with torch.cuda.stream(made or torch.cuda.default_stream()):
+                    torch.cuda._sleep(1_000_000)   # (what does not wait for the forwards is ahead of them)
+                ses.step(Params(seed=4, step=step))
+            torch.cuda.synchronize()
+            seen = [t.clone() for t in (ses.st.block_tokens, ses.kv.entries, ses.kv.seq_len, ses.d.logits, ses.kv.mass, ses.kv.position)]
+        torch.cuda.synchronize()
+        runs.append(seen)
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
