@@ -231,12 +231,21 @@ def s2d2_kv4_evict(kv: Kv4Cache, budget: int, slack: int = 0, sink: int = 0, rec
     kv._call(lib.s2d2_kv4_evict, stream, kv.N, budget, slack, sink, recent, _ptr(moves), 0 if moves is None else moves.numel())
 
 
+def _release(held, stream):
+    """Scratch and lse of an attachment that ended: their memory is free when the engine's stream is done with them."""
+    for t in (held or (None,))[1:]:
+        if t is not None:
+            t.record_stream(stream)
+
+
 def s2d2_set_kv4(eng, kv: Optional[Kv4Cache]):
     """Attaches the cache to the engine's context (None: detaches): from now on its calls take `kv` where they take a KvCache."""
     lib = _lib()
+    held = getattr(eng, "_kv4", None)
     if kv is None:
         _check(lib, lib.s2d2_set_kv4(eng.ctx, None, None, 0, None))
         eng._kv4 = None
+        _release(held, eng.stream)
         return
     if kv.device != torch.device(eng.device.type, eng.device.index or 0) or kv.N > eng.max_batch:
         _refuse(f"a cache of {kv.N} sequences on {kv.device} does not fit an engine of {eng.max_batch} on {eng.device}")
@@ -246,3 +255,4 @@ def s2d2_set_kv4(eng, kv: Optional[Kv4Cache]):
     lse = torch.empty(eng.stage_rows, heads, device=kv.device) if kv.mass is not None else None
     _check(lib, lib.s2d2_set_kv4(eng.ctx, kv._ref, scratch.data_ptr(), need, _ptr(lse)))
     eng._kv4 = (kv, scratch, lse)   # alive while the context uses them
+    _release(held, eng.stream)

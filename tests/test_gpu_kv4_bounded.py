@@ -168,3 +168,22 @@ def test_eviction_runs_on_the_stream_of_the_forwards():
         runs.append(seen)
     for other in runs[1:]:
         assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+
+
+def test_the_scratch_of_a_detached_cache_is_not_handed_out_while_it_is_used():
+    cfg = SMALL_BF16
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ses = Session(cfg, I.gen_weights(cfg, 3), 1, 4, 4096, cache_bits=4, budget=64)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(None):
+        s2d2_set_kv4(ses.eng, ses.kv)            # (a scratch of the default stream's memory, used on the engine's)
+        torch.cuda.synchronize()
+        old = [t.data_ptr() for t in ses.eng._kv4[1:]]
+        sizes = [t.numel() * t.element_size() for t in ses.eng._kv4[1:]]
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(50_000_000)        # the engine's stream is busy for a while
+        s2d2_set_kv4(ses.eng, None)
+        new = [torch.empty(s, dtype=torch.uint8, device=DEV) for s in sizes]
+        assert not set(old) & {t.data_ptr() for t in new}
+    torch.cuda.synchronize()
