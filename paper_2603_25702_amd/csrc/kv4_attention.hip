@@ -24,7 +24,8 @@ namespace s2d2 {
 // 2^15: most tiles need no maximum and rescale nothing, and half keeps 11 bits of a weight down to 2^-21 of the largest and 2^-32 of it below (with the maximum itself as the
 // reference a million entries of 2^-24 each would lose a tenth of their weights).  Sums are in 32 bits.
 // Operands of more than 16 bits (fp32 models; queries in two planes) are split into planes of bf16, whose products are exact in 32 bits: 3
-// planes hold the 24 bits of a float.  Softmax weights are half (11 bits; off by at most 2^-12 of the weight), of fp32 models two half planes.
+// planes hold the 24 bits of a float.  Softmax weights are half (11 bits; off by at most 2^-12 of the weight); of fp32 models three planes of bf16, V then goes
+// through LDS as bf16.
 // The window's own rows, a few tiles, take the same way with K in the caller's type and V, weights in planes of bf16.
 // Measured (us, head dimension 128): 16 sequences x 32 rows x 32 heads on 8 over 8192 entries, 97 (69 GFLOP at 700 TFLOP/s; the vector instructions
 // bound it: about 281 beside 32 matrix instructions for 64 rows x 32 keys, on two wavefronts a SIMD); 4 x 1 row over 60000 to 65536 entries, 55
@@ -40,11 +41,11 @@ constexpr int waves_of(int D) { return D == 256 ? 4 : 8; }
 constexpr int min_run_of(int D) { return 4 * waves_of(D); }   // tiles of a split, at least: four a wavefront (a join costs a launch of 4 to 5 us)
 
 template <int QM> struct Mode;
-// QP: planes of the queries; PP: of the softmax weights on cached values (half); WP: of the window's keys and values; WPP: of the weights on them (bf16)
+// QP: planes of the queries; PP: of the softmax weights on cached values (half; of fp32 models bf16); WP: of the window's keys and values; WPP: of the weights on them (bf16)
 template <> struct Mode<Q_BF16> { typedef bf16_t T; static constexpr int QP = 1, PP = 1, WP = 1, WPP = 2; };
 template <> struct Mode<Q_BF16X2> { typedef bf16_t T; static constexpr int QP = 2, PP = 1, WP = 1, WPP = 2; };
 template <> struct Mode<Q_F16> { typedef bf16_t T; static constexpr int QP = 1, PP = 1, WP = 1, WPP = 2; };
-template <> struct Mode<Q_F32> { typedef float T; static constexpr int QP = 3, PP = 2, WP = 3, WPP = 3; };
+template <> struct Mode<Q_F32> { typedef float T; static constexpr int QP = 3, PP = 3, WP = 3, WPP = 3; };
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_t;
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
     const bool part = tile * 32 + 32 > sq.S;
     if (part && tile * 32 + kperm >= sq.S) v.clear();   // (what lies behind the entries may be anything)
 #pragma unroll
-    for (int i = 0; i < DS; ++i) v_word(i) = codes_f16(v.w[i], v.scale(i));
+    for (int i = 0; i < DS; ++i) v_word(i) = QM == Q_F32 ? codes_bf16(v.w[i], v.scale(i)) : codes_f16(v.w[i], v.scale(i));
     lds_written();
     after_v();
     __builtin_amdgcn_s_setprio(1);
@@ -403,18 +404,17 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
       st[t].weights(s[t], a.scale_log2e, p);
 #pragma unroll
       for (int j = 0; j < 2; ++j)
+        if constexpr (QM == Q_F32) {   // (half planes would end at 2^-24: 2^-31 of the largest weight, and their low bits before that)
+          const float x[8] = {p[8 * j], p[8 * j + 1], p[8 * j + 2], p[8 * j + 3], p[8 * j + 4], p[8 * j + 5], p[8 * j + 6], p[8 * j + 7]};
+          split8<PP>(x, pw[t][j]);
+        } else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = p[8 * j + 2 * i], y = p[8 * j + 2 * i + 1];
-#pragma unroll
-          for (int e = 0; e < PP; ++e) {
+          for (int i = 0; i < 4; ++i) {
             f16x2_t hv;
-            hv[0] = (_Float16)x;
-            hv[1] = (_Float16)y;
-            pw[t][j][e][i] = __builtin_bit_cast(uint32_t, hv);
-            if (e + 1 < PP) { x -= (float)hv[0]; y -= (float)hv[1]; }
+            hv[0] = (_Float16)p[8 * j + 2 * i];
+            hv[1] = (_Float16)p[8 * j + 2 * i + 1];
+            pw[t][j][0][i] = __builtin_bit_cast(uint32_t, hv);
           }
-        }
     }
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-          for (int e = 0; e < PP; ++e) st[t].o[dt] = mfma_f16(vf, pw[t][j][e], st[t].o[dt]);
+          for (int e = 0; e < PP; ++e) st[t].o[dt] = QM == Q_F32 ? mfma_bf16(vf, pw[t][j][e], st[t].o[dt]) : mfma_f16(vf, pw[t][j][e], st[t].o[dt]);
       }
     __builtin_amdgcn_s_setprio(0);
     lds_read();
