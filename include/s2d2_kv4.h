@@ -63,7 +63,7 @@ typedef struct {
  *   out     [rows, n_q_heads, head_dim] in `dtype`, out_stride elements from row to row.  A row that sees nothing: 0
  *   lse     [rows, n_q_heads] fp32 or NULL: natural logarithm of the sum of exp(score); -inf for a row that sees nothing
  * q, k, v, out are 16-byte aligned, their strides whole 16 bytes.  A window row with a NaN or an infinity in v makes the rows that see it NaN,
- * and no others.  S2D2_F32: products and sums as in 32 bits; S2D2_BF16: products of bf16 queries, softmax weights in half, sums in 32 bits. */
+ * and no others; finite values of v up to 2^100 in magnitude do not overflow (the largest weight of a row stands for 2^7 to 2^15 in sums of 32 bits).  S2D2_F32: products and sums as in 32 bits; S2D2_BF16: products of bf16 queries, softmax weights in half, sums in 32 bits. */
 typedef struct {
   int32_t N, T, rows, n_q_heads, dtype;
   float scale;

@@ -88,17 +88,20 @@ __device__ __forceinline__ u32x4_t codes_for(uint32_t w, float s) { return QM ==
 template <int QM>
 __device__ __forceinline__ f32x16_t score_mfma(const u32x4_t& a, const u32x4_t& b, const f32x16_t& c) { return QM == Q_F16 ? mfma_f16(a, b, c) : mfma_bf16(a, b, c); }
 
-// 8 values as P planes of bf16 whose sum is the value (P = 3: exactly, above the subnormals)
-template <int P>
+// 8 values as P planes of bf16 whose sum is the value (P = 3: exactly, above the subnormals).  WIDE: finite values above bf16's largest, 3.39e38, too, which
+// would round to infinity: the first plane is cut to it and the others take the rest (an infinity or a NaN is a NaN in the last plane then).
+static constexpr float BF16_MAX = 3.38953139e38f;
+template <int P, bool WIDE = false>
 __device__ __forceinline__ void split8(const float (&x)[8], u32x4_t (&p)[P]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float a = x[2 * i], b = x[2 * i + 1];
 #pragma unroll
     for (int k = 0; k < P; ++k) {
+      const bool cut = WIDE && k == 0;
       bf16x2_t h;
-      h[0] = (__bf16)a;
-      h[1] = (__bf16)b;
+      h[0] = (__bf16)(cut ? __builtin_amdgcn_fmed3f(a, -BF16_MAX, BF16_MAX) : a);
+      h[1] = (__bf16)(cut ? __builtin_amdgcn_fmed3f(b, -BF16_MAX, BF16_MAX) : b);
       p[k][i] = __builtin_bit_cast(uint32_t, h);
       if (k + 1 < P) { a -= (float)h[0]; b -= (float)h[1]; }
     }
@@ -115,7 +118,7 @@ template <int P>
 __device__ __forceinline__ void load_planes(const float* p, int, u32x4_t (&r)[P]) {
   const f32x4_t a = ((const f32x4_t*)p)[0], b = ((const f32x4_t*)p)[1];
   const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  split8<P>(x, r);
+  split8<P, true>(x, r);
 }
 
 // ---- the batch as runs of key tiles ----
@@ -451,7 +454,7 @@ __global__ __launch_bounds__(64 * waves_of(D)) void kv4_attention_kernel(const K
       u32x4_t v[WP];
       load_planes<WP>((const T*)a.v + at + 8 * ds, 0, v);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= (v[0][i] & 0x7f80u) == 0x7f80u || (v[0][i] & 0x7f800000u) == 0x7f800000u;
+      for (int i = 0; i < 4; ++i) bad |= (v[WP - 1][i] & 0x7f80u) == 0x7f80u || (v[WP - 1][i] & 0x7f800000u) == 0x7f800000u;
       v_word(ds) = there ? v[0] : u32x4_t{0, 0, 0, 0};
     }
     bad |= (bool)__shfl_xor((int)bad, 32, 64);

@@ -1,4 +1,4 @@
-"""fp32 rows on the 4-bit cache keep the bits of fp32, in weights far below the largest too; heads and rows beside those that are NaN.
+"""fp32 rows on the 4-bit cache keep the bits of fp32: weights far below the largest, finite values up to the type's largest; and rows beside those that are NaN.
 
 Error bound of fp32 rows, relative to sum p |v|: a score is a sum of D products in 32 bits, off by at most D * 2^-24 * sum |q||k| times scale; scaling and exponent
 add 4 * 2^-24 of the same magnitude and 2^-21; weights relative to their sum are off by twice that.  Weights are split into three planes of bf16: 2^-24 of each, whatever its size.  Sums of n terms: sqrt(n) * 2^-24 * 8; the output 2^-21.
@@ -61,6 +61,48 @@ def test_fp32_rows_of_flat_and_peaked_weights(hq, hkv, d, page, scale):
     case.scale = scale
     case.make()
     check_fp32(case.run())
+
+
+def test_finite_values_up_to_the_largest():
+    """Window rows of fp32 beyond bf16's largest value, 3.39e38, and queries against small keys; values of up to 2^100 of rows that are seen in full."""
+    big = 3.4e38
+    case = Case([40], [4], 2, 2, 64, 16, F32, "causal", seed=8)
+    case.k[1, 0, 5] = big           # rows 1, 2, 3 see it: 8 of their scores
+    case.q[:, 0, 5] = 2.0 ** -125
+    case.make()
+    check_fp32(case.run())
+    case = Case([40], [4], 2, 2, 64, 16, F32, "causal", seed=9)
+    case.q[2, 1, 7] = -big          # against keys that are 0 there
+    case.k[:, 1, 7] = 0
+    c = case.cache
+    c.k[0][0][:, 1, :32] = 0
+    pages, slots = c.places(0, 40)
+    c.c.k_codes[0, torch.from_numpy(pages), 1, torch.from_numpy(slots), :16] = 0
+    case.make()
+    check_fp32(case.run())
+    for dtype in (BF, F32):
+        case = Case([40], [4], 2, 2, 64, 16, dtype, "causal", seed=10)
+        case.v.mul_(2.0 ** 98)
+        case.make()
+        case.run().check()
+
+
+def test_a_finite_value_above_bf16_s_largest_is_no_infinity():
+    case = Case([0], [3], 1, 1, 32, 16, F32, "causal", seed=11)
+    case.q.fill_(1.0)
+    case.k.fill_(0.0)
+    case.k[1] = -3.0                # its weight in rows 1 and 2 against row 0's: exp(-96 * scale)
+    case.scale = 0.5
+    case.v.fill_(1.0)
+    case.v[1] = 3.4e38
+    case.k[2] = -100.0
+    case.make()
+    case.run()
+    out, lse, absout, most = case.want()
+    got = case.out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    rel = 2 * (most[..., None] * 36 * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -20
+    assert (np.abs(got - out) <= rel * absout).all()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
