@@ -59,7 +59,7 @@ typedef struct {
  *   k, v    [rows, n_kv_heads, head_dim] in `dtype`, kv_stride elements from row to row: the window's own keys (after
  *           rotation) and values; both NULL: the rows see the cached entries only
  *   lo, hi  [rows] or both NULL: row r sees the rows [lo[r], hi[r]) of its sequence's window, and itself; NULL: the rows up to itself
- *   scale   > 0; scores are scale * q.k
+ *   scale   > 0, at most 2.35e38; scores are scale * q.k
  *   out     [rows, n_q_heads, head_dim] in `dtype`, out_stride elements from row to row.  A row that sees nothing: 0
  *   lse     [rows, n_q_heads] fp32 or NULL: natural logarithm of the sum of exp(score); -inf for a row that sees nothing
  * q, k, v, out are 16-byte aligned, their strides whole 16 bytes.  A window row with a NaN or an infinity in v makes the rows that see it NaN,

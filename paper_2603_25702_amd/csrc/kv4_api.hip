@@ -76,7 +76,7 @@ int32_t attn_args(const s2d2_kv4_view* kv, int32_t layer, const s2d2_kv4_rows* r
   if (!r) return fail(S2D2_EINVAL, "rows are NULL");
   if ((rc = check_batch(r->N, r->T, 8192)) || (rc = check_dtype(r->dtype)) || (rc = check_q_heads(kv, r->n_q_heads)) || (rc = check_keys(kv, r->N, r->T, r->n_q_heads))) return rc;
   if (r->rows < 1) return fail(S2D2_EINVAL, "rows=%d must be positive", r->rows);
-  if (!(r->scale > 0.f) || r->scale > 3e38f) return fail(S2D2_EINVAL, "scale must be positive and finite");
+  if (!(r->scale > 0.f) || r->scale > 2.35e38f) return fail(S2D2_EINVAL, "scale must be positive and at most 2.35e38 (scores are taken to base 2: scale * 1.4427 must be finite)");
   if (!r->q || !r->row0 || !r->n_rows) return fail(S2D2_EINVAL, "q, row0 or n_rows is NULL");
   const int64_t width = (int64_t)r->n_q_heads * kv->head_dim;
   if (((uintptr_t)r->q & 15) || !stride_ok(r->q_stride, width, r->dtype)) return fail(S2D2_EINVAL, "q must be 16-byte aligned, its row stride whole 16 bytes and at least %lld elements", (long long)width);
