@@ -469,7 +469,9 @@ int32_t forward(s2d2_ctx* c, const s2d2_kv_view* kv, int32_t N, const FwdSize& s
       x.row0 = c->plan.seq_row0; x.n_rows = c->plan.seq_rows; x.lo = c->plan.row_lo; x.hi = c->plan.row_hi;
       x.out = c->obuf; x.o_ld = ld_o; x.o_lo = lo_o; x.lse = weigh ? c->kv4_lse : nullptr;
       x.scale_log2e = 1.44269504088896340736f / sqrtf((float)d.head_dim);
-      { ProfScope ps(c, 1, 0.0); launch_kv4_attention(st, mode4, x, l, c->kv4_scratch); }
+      bool join;
+      { ProfScope ps(c, 1, 0.0); join = launch_kv4_attention(st, mode4, x, l, c->kv4_scratch); }
+      if (join) { ProfScope ps(c, 1, 0.0); launch_kv4_merge(st, mode4, x); }
       x.row_mass = weigh ? c->kv4_row_mass + (size_t)l * c->rows_cap * d.n_kv_heads : nullptr;
       if (weigh) { ProfScope ps(c, 1, 0.0); launch_kv4_weigh(st, mode4, x, l); }
       if (LR == 0 && l == d.n_layers - 1) return check_launch("forward");

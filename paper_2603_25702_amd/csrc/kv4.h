@@ -61,6 +61,7 @@ struct Kv4Attn {
   int2* part_of;     // [N] of a sequence with several splits: its first item, its splits
   int32_t expect;    // rows that a sequence is expected to have (at most T): what the splits are chosen for
   int32_t groups;    // groups of query tiles of T rows
+  int32_t q_tiles, per_wg;   // query tiles of T rows, and of a workgroup
   int32_t items;     // (sequence, split) pairs the grid holds
   int32_t per_item;  // workgroups of one with the expected rows: KV heads * groups of query tiles
   int32_t room;      // splits beyond one a sequence that the scratch holds
@@ -72,7 +73,8 @@ struct Kv4Attn {
 
 // Queries and window rows: bf16; bf16 queries in two planes; queries and window keys as half values; fp32
 enum Kv4Query { Q_BF16 = 0, Q_BF16X2 = 1, Q_F16 = 2, Q_F32 = 3 };
-void launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void* scratch);
+bool launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void* scratch);   // whether a sequence may have several splits, for launch_kv4_merge to join
+void launch_kv4_merge(hipStream_t st, int mode, const Kv4Attn& a);
 size_t kv4_attention_bytes(const Kv4& kv, int N, int T, int Hq);
 void launch_kv4_weigh(hipStream_t st, int mode, Kv4Attn& a, int layer);
 int kv4_evict_init();

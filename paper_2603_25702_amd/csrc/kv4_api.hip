@@ -140,7 +140,8 @@ int32_t s2d2_kv4_attention(void* stream, const s2d2_kv4_view* kv, int32_t layer,
   if (scratch_bytes < need) return fail(S2D2_ENOSPC, "scratch has %zu bytes, %zu needed", scratch_bytes, need);
   if (need && (!scratch || ((uintptr_t)scratch & 15))) return fail(S2D2_EINVAL, "scratch is NULL or not 16-byte aligned");
   if ((rc = kv4_ready())) return rc;
-  launch_kv4_attention((hipStream_t)stream, rows->dtype == S2D2_F32 ? Q_F32 : Q_BF16, a, layer, scratch);
+  const int mode = rows->dtype == S2D2_F32 ? Q_F32 : Q_BF16;
+  if (launch_kv4_attention((hipStream_t)stream, mode, a, layer, scratch)) launch_kv4_merge((hipStream_t)stream, mode, a);
   return check_launch("s2d2_kv4_attention");
 }
 

@@ -883,7 +883,6 @@ template <int D, int QM, int QT>
 static void launch_attn(hipStream_t st, const Kv4Attn& a, int layer, const AttnShape& s) {
   const int wgs = (a.items * a.kv.H + 7) / 8 * 8 * s.groups;
   S2D2_LAUNCH((kv4_attention_kernel<D, QM, QT>), dim3(wgs), dim3(64 * waves_of(D)), (attn_lds<D, QT>()), st, a, layer);
-  if (s.most > 1) S2D2_LAUNCH((kv4_merge_kernel<D, QM>), dim3(a.N * a.kv.H * s.q_tiles * (D / 32)), dim3(256), 0, st, a, s.q_tiles, s.per_wg);
 }
 
 template <typename F>
@@ -894,7 +893,7 @@ static void by_head_dim(int D, const F& f) {
   else f(std::integral_constant<int, 256>{});
 }
 
-void launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void* scratch) {
+bool launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void* scratch) {
   const AttnShape s = shape_of(a.kv, mode, a.N, a.T, a.expect, a.Hq, a.k != nullptr);
   a.items = s.items;
   a.per_item = s.per_item;
@@ -902,6 +901,8 @@ void launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void*
   a.room = s.room;
   a.target = TARGET;
   a.min_run = min_run_of(a.kv.D);
+  a.q_tiles = s.q_tiles;
+  a.per_wg = s.per_wg;
   const size_t slots = (size_t)((s.items * a.kv.H + 7) / 8 * 8) * s.groups * s.per_wg;
   a.part_o = (float*)scratch;
   a.part_ml = a.part_o + slots * 32 * a.kv.D;
@@ -915,6 +916,16 @@ void launch_kv4_attention(hipStream_t st, int mode, Kv4Attn& a, int layer, void*
     else if (mode == Q_F16) launch_attn<D, Q_F16, 1>(st, a, layer, s);
     else if (s.per_wg == 2) launch_attn<D2, Q_BF16, 2>(st, a, layer, s);
     else launch_attn<D, Q_BF16, 1>(st, a, layer, s);
+  });
+  return s.most > 1;
+}
+
+void launch_kv4_merge(hipStream_t st, int mode, const Kv4Attn& a) {
+  by_head_dim(a.kv.D, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    const dim3 grid(a.N * a.kv.H * a.q_tiles * (D / 32)), wg(256);
+    if (mode == Q_F32) S2D2_LAUNCH((kv4_merge_kernel<D, Q_F32>), grid, wg, 0, st, a, a.q_tiles, a.per_wg);
+    else S2D2_LAUNCH((kv4_merge_kernel<D, Q_BF16>), grid, wg, 0, st, a, a.q_tiles, a.per_wg);
   });
 }
 
