@@ -114,8 +114,8 @@ int64_t s2d2_kv4_evict_bytes(const s2d2_kv4_view* kv, int32_t N);
 
 /* From this call on the calls of s2d2.h on `ctx` that take an s2d2_kv_view keep the prefix in this cache (NULL: in the view's own pages again).
  * Their views then have to describe it: k_pages = k_codes, v_pages = v_codes, the same page_table, seq_len, n_pages, page_size and
- * max_pages_per_seq (else S2D2_EINVAL).  n_layers, n_kv_heads and head_dim must be the model's.  Rows of a window are attended to at the model's
- * precision and quantised when they are appended.  With mass, s2d2_verify, s2d2_prefill and s2d2_block_complete add the weights of their windows' rows
+ * max_pages_per_seq (else S2D2_EINVAL).  n_layers, n_kv_heads and head_dim must be the model's.  Rows of a window are attended to as
+ * the model's operand mode has them (by default queries and window keys as half: 11 bits, up to 65504; act_planes 1, 2: bf16 queries of one or two planes, bf16 keys) and quantised when they are appended.  With mass, s2d2_verify, s2d2_prefill and s2d2_block_complete add the weights of their windows' rows
  * (the drafting forward adds none), to the cached entries and to the rows that they see among themselves: the context's next append enters its rows with the mass
  * that the last of these forwards gave them (0 if there was none since this call).  s2d2_kv4_evict on the same cache may follow an append at any time: positions go by seq_len.
  * lse: device [s2d2_stage_rows(max_batch, max_block), n_q_heads] fp32, needed with mass; scratch: device, 16-byte aligned, at least

@@ -27,16 +27,18 @@ namespace s2d2 {
 // planes hold the 24 bits of a float.  Softmax weights are half (11 bits; off by at most 2^-12 of the weight); of fp32 models three planes of bf16, V then goes
 // through LDS as bf16.
 // The window's own rows, a few tiles, take the same way with K in the caller's type and V, weights in planes of bf16.
-// Measured (us, head dimension 128): 16 sequences x 32 rows x 32 heads on 8 over 8192 entries, 97 (69 GFLOP at 700 TFLOP/s; the vector instructions
-// bound it: about 281 beside 32 matrix instructions for 64 rows x 32 keys, on two wavefronts a SIMD); 4 x 1 row over 60000 to 65536 entries, 55
-// (283 MB at 5.1 TB/s, a large copy's rate); 1 x 1 row over 512 entries, 12 (launch, dependent loads, the join of the wavefronts).
+// Measured (us, head dimension 128): 16 sequences x 32 rows x 32 heads on 8 over 8192 entries, 98 (69 GFLOP at 700 TFLOP/s).  By its counters the vector
+// instructions issue in 51 % of that time and the matrix cores are busy in 36 %, while a wavefront waits for 39 % of its life: the chain of a tile (V
+// into LDS, scores, softmax, V back) with two wavefronts a SIMD to cover it.  4 x 1 row over 60000 to 65536 entries, 55 (283 MB at 5.1 TB/s, read from three caches in
+// turn, more than the memory-side cache holds; a copy of 4 GiB reads and writes 4.7); 1 x 1 row over 512 entries, 12 (launch, dependent loads, the join of the
+// wavefronts).  fp32 rows: the 16 x 32 rows 228; with their weights in two half planes, which lose the small ones, 200.
 // ---------------------------------------------------------------------------------------------
 static constexpr float LN2 = 0.69314718055994530942f;
 static constexpr float LOWEST = -3.402823466e38f;   // reference of a row that has seen nothing
 static constexpr float BELOW = 7.f;                 // a reference is taken this far below a maximum (base 2)
 static constexpr float MOST = 32768.f;              // and moves when the weights of a tile of keys sum up to more
-// Wavefronts of a workgroup, one workgroup a compute unit.  With four of them and 512 registers the 16 x 32 rows over 8192 entries took 146 us beside 111,
-// with three wavefronts a SIMD at 168 registers, which spill, 152: two that keep to their registers hide each other's waits.  Heads of 256 take 128 registers for the output alone: four wavefronts of up to 512 registers, else eight of up to 256.
+// Wavefronts of a workgroup, one workgroup a compute unit: two a SIMD cover each other's waits.  A pass by four / eight of them: 16 x 32 rows over 8192 entries
+// 139 / 104 us, 4 x 1 row over 60000 to 65536 86 / 62, 1 x 1 row over 512 20 / 12.  Heads of 256 take 128 registers for the output alone: four wavefronts of up to 512 registers, else eight of up to 256.
 constexpr int waves_of(int D) { return D == 256 ? 4 : 8; }
 constexpr int min_run_of(int D) { return 4 * waves_of(D); }   // tiles of a split, at least: four a wavefront (a join costs a launch of 4 to 5 us)
 
@@ -663,8 +665,9 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(const Kv4Attn a, int til
 // wavefront every fourth pair of them.  Scores are computed as S = Q K^T, so that a lane owns a key and the sum over rows stays in it; the queries
 // lie in LDS in operand order, up to QC tiles of 32 rows at a time, each read for two tiles of keys.  The sums of a pair over these rows are
 // added to the mass by one lane a key, tile of rows after tile of rows: a fixed order.
-// Bound: the exponentials (16 cycles each, with a multiply-add and an add 24 for 64 scores); the matrix instructions of a tile take 256 cycles beside
-// 384 of these.  16 x 32 rows x 32 heads on 8 over 8192 entries of 128: 50 us (34 GFLOP, 690 TFLOP/s); with two workgroups a compute unit instead of three 62.
+// 16 x 32 rows x 32 heads on 8 over 8192 entries of 128: 50 us (34 GFLOP, 690 TFLOP/s).  By its counters the vector instructions issue in 69 % of that
+// time (an exponential takes 16 cycles, with a multiply-add and an add 24 for 64 scores) and the matrix cores are busy in 39 %: partly beside each other, on three
+// wavefronts a SIMD, each of which waits for 47 % of its life.  A pass with two workgroups a compute unit instead of three: 57 us for 51.
 // ---------------------------------------------------------------------------------------------
 static constexpr int WEIGH_WAVES = 4;
 template <int D, int QM>
@@ -674,7 +677,7 @@ static constexpr size_t weigh_lds() { return (size_t)QC<D, QM> * (32 * D * 2 * M
 
 // The weights that a window's rows give each other, into row_mass: a workgroup has one sequence, one KV head and 32 keys, a wavefront every fourth tile of
 // 32 query rows that sees one of them (of a causal window half the tiles).  S = Q K^T as below, keys and queries from memory; the wavefronts' sums are added up
-// in their order.  Verification windows of 16 x 32 rows have 128 of these workgroups beside the 768 of their cached entries, in one launch.
+// in their order.  In one launch with the cached entries: a layer of 16 x 32 rows behind 8192 takes 54 us, 53 without the window's 128 workgroups.
 template <int D, int QM>
 __device__ __forceinline__ void weigh_window(const Kv4Attn& a, int block, uint8_t* s_mem) {
   typedef typename Mode<QM>::T T;
@@ -846,7 +849,7 @@ static constexpr int WEIGH_TARGET = 768, WEIGH_MIN_RUN = 16;   // three workgrou
 static constexpr int TARGET = 256;   // workgroups that are resident at once: one a compute unit (eight wavefronts of up to 256 registers)
 
 // Query tiles per workgroup: two share the conversion of K and V; one where there is no second, and where two would not leave registers (outputs of
-// heads of 256, planes of queries).  16 x 32 rows x 4 heads over 8192 entries: 139 us by one, 111 by two in the same build (97 now).
+// heads of 256, planes of queries).  A pass of 16 x 32 rows x 4 heads over 8192 entries: 130 us by one, 104 by two.
 static int tiles_per_wg(int D, int mode, int q_tiles) { return D <= 128 && (mode == Q_BF16 || mode == Q_F16) && q_tiles >= 2 ? 2 : 1; }
 
 struct AttnShape { int q_tiles, per_wg, groups, per_item, items, most, room; };

@@ -1,6 +1,6 @@
 // The 4-bit cache: quantising append, entries read back, eviction by gathered attention weight.
-// Format and semantics: include/s2d2_kv4.h.  Append, read and move take few operations a byte (24 MB, 5 us at a copy's rate, take 11: the start and end of a
-// launch that short); picking is bound by its passes over a list.
+// Format and semantics: include/s2d2_kv4.h.  Append, read and move take few operations a byte; 24 MB, 5 us at a copy's rate, take 10 to 12 (each workgroup makes one pass
+// behind a chain of counts, entries and page table).  Picking makes several passes over a list.
 #include "kv4.h"
 
 #include <algorithm>
@@ -23,7 +23,7 @@ Kv4 kv4_of(const s2d2_kv4_view* view) {
 // Append.  A thread takes 8 values of a row (a 16-byte load of bf16), four neighbours make a group: the group's largest |x| goes round
 // by two DPP moves as an integer (the bits of |x| order as |x| does, with NaN above infinity above all else), v_cvt_scalef32_pk_fp4_f32
 // rounds x / 2^e to nearest-even codes.
-// 36 layers x 16 sequences of up to 16 rows, 8 heads of 128, bf16: 11.5 us; 8 layers x 4 of up to 192 rows, fp32: 10.0.  The counts follow in a launch of
+// 36 layers x 16 sequences of up to 16 rows, 8 heads of 128, bf16: 12 us; 8 layers x 4 of up to 192 rows, fp32: 9.5.  The counts follow in a launch of
 // their own (2 to 4 us): a row's place depends on the count that every workgroup of the first one reads.
 // ---------------------------------------------------------------------------------------------
 static constexpr int APPEND_ROWS = 4;   // rows of a sequence per workgroup, all in flight at once
@@ -123,7 +123,7 @@ void launch_kv4_append(hipStream_t st, int dtype, const Kv4& kv, int N, const Kv
 }
 
 // ---------------------------------------------------------------------------------------------
-// Entries read back: 8 values a thread of each of READ_ROWS entries.  11 us for the rows of either append above.
+// Entries read back: 8 values a thread of each of READ_ROWS entries.  10.5 us for the rows of either append above.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 static constexpr int READ_ROWS = 4;
@@ -188,11 +188,13 @@ void launch_kv4_read(hipStream_t st, int dtype, const Kv4& kv, int N, int T, con
 // A wavefront owns a run of consecutive entries where ranks are needed: its counts go through LDS once, ranks inside it come from ballots.
 // kv4_move_kernel: the moves of all lists by as many workgroups as there are compute units for.  Places that are written lie below the budget,
 // places that are read behind it, so the moves need no order among themselves; and a list that is a little too long moves a few entries only.
-// 512 lists of 4160 entries to 4096: 32 us to pick, 7 to move; 32 lists of 32768 to 4096: 69 and 16 (262 us when the picking workgroups moved as
-// well: 32 compute units of 256).  Picking is bound by one compute unit's passes over its list.
+// 512 lists of 4160 entries to 4096: 33 us to pick, 7 to move; 32 lists of 32768 to 4096: 69 and 15.  The 512 lists are one round of workgroups, two a compute
+// unit: vector instructions issue in 52 % of the time, a wavefront waits (barriers, LDS, memory) for 61 % of its life.  The 32 long lists keep 32 of 256 compute units busy.
 // ---------------------------------------------------------------------------------------------
 static constexpr int EVICT_KEYS = 36864;   // keys kept in LDS (144 KB); those of longer lists are formed again from memory
-static constexpr int PICK_SHORT = 8192;    // lists up to here by eight wavefronts, two workgroups a compute unit: a pass over the 512 lists 48 us, by sixteen 51, by four 62
+// Lists up to here by eight wavefronts, two workgroups a compute unit.  Both launches, us, by eight / sixteen: 4608 lists of 4160 entries (36 layers) 179 / 246, 512 of them 30 / 35, 1024 of
+// 600 25 / 39, 32 of 1000 16 / 18; few long ones the other way, 256 of 8192 34 / 28; by four, 512 of 4160 take a fifth longer than by eight.
+static constexpr int PICK_SHORT = 8192;
 static constexpr int EVICT_AHEAD = 4;      // entries or moves that a thread has in flight
 
 __device__ __forceinline__ uint32_t evict_key(float mass, int position, int sink, int tail) {
