@@ -11,7 +11,7 @@ import torch
 
 import s2d2_inputs as I
 from oracle import s2d2_oracle as O
-from paper_2603_25702_amd import Params, s2d2_kv4_read
+from paper_2603_25702_amd import Params, s2d2_kv4_read, s2d2_set_kv4
 from paper_2603_25702_amd.runner import Session
 from tests.test_gpu_kv4_session import Run, i32
 from tests.test_gpu_parity import SMALL_BF16, TINY
@@ -162,3 +162,15 @@ def test_entries_of_a_later_chunk_win_by_their_weight():
             assert set(position[sure]) <= set(now[:, h]) and not set(position[never]) & set(now[:, h])
             later += int((now[:, h] >= T).sum())
     assert later > 0
+
+
+def test_rows_that_no_forward_weighed_since_the_cache_was_attached_bring_nothing():
+    cfg = TINY
+    run = Run(cfg, [40, 20], 4, seed=3, budget=1000)
+    run.step(Params(seed=5), advance=False, append=False)
+    run.a.n_accept.copy_(run.d.span_len)
+    s2d2_set_kv4(run.eng, run.kv)
+    assert (run.append_checked() > 0).all()
+    for n, s in enumerate((40, 20)):
+        m = masses(run.kv, n)
+        assert (m[:s] > 0).all() and (m[s:] == 0).all()
