@@ -225,7 +225,8 @@ def s2d2_kv4_weigh(kv: Kv4Cache, layer: int, rows: Kv4Rows, stream: Optional[tor
 
 
 def s2d2_kv4_evict(kv: Kv4Cache, budget: int, slack: int = 0, sink: int = 0, recent: int = 0, stream: Optional[torch.cuda.Stream] = None):
-    """Cuts the sequences with more than budget + slack entries to `budget` of them, list by list; the scratch is the cache's own."""
+    """Cuts the sequences with more than budget + slack entries to `budget` of them, list by list; the scratch is the cache's own.  Entries of
+    s2d2_kv4_append that no rows have been weighed against yet stand at 0: protect them by `recent`."""
     lib = _LIB or _lib()
     moves = kv.moves
     kv._call(lib.s2d2_kv4_evict, stream, kv.N, budget, slack, sink, recent, _ptr(moves), 0 if moves is None else moves.numel())
